@@ -23,7 +23,14 @@
  *                    III-C, Alg. 1, Eqs. (6)-(11)): per-request verify
  *                    lengths under the shared budget, the offsets that
  *                    dsv_verify_attn and dsv_accept read as cu_qlens, and the
- *                    packed token, position and cache-reference rows.
+ *                    packed token, position and cache-reference rows;
+ *   dsv_rope_append  rotary positions on a step's q and k, and its k and v
+ *                    written to the paged cache, in bf16 or quantised to 8 bits
+ *                    (dsv_kv_read reads rows of either cache back);
+ *   dsv_tree_attn, dsv_tree_accept, dsv_tree_commit
+ *                    verify attention, greedy acceptance and the cache update of
+ *                    a drafted tree in place of a block (dsv_tree_masks makes
+ *                    the masks and positions of a tree from its parents).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -69,13 +76,16 @@ typedef enum {
                             /* no-allocation entry point                       */
 } dsv_status;
 
-typedef enum { DSV_F32 = 0, DSV_BF16 = 1 } dsv_dtype;
+/* DSV_FP8: 8-bit e4m3 codes (no infinities, largest finite value 448). */
+typedef enum { DSV_F32 = 0, DSV_BF16 = 1, DSV_FP8 = 2 } dsv_dtype;
 
 /* Largest verify length per request: one anchor plus 15 candidates (Sec. II). */
 #define DSV_MAX_QLEN 16
 /* Tokens per KV page.  The paper cites paged attention without fixing a page
  * size; the library supports exactly 16. */
 #define DSV_PAGE_SIZE 16
+/* Largest drafted tree per request, its root (the anchor) included. */
+#define DSV_MAX_NODES 64
 
 /*
  * Dimensions of one verify_attn call.  All fields are host values.
@@ -383,6 +393,215 @@ int dsv_dvl_allocate_pack(const float *pred_logits, const int32_t *num_live,
                           int32_t *packed_positions, int32_t *packed_kv_refs,
                           float *scores_out, int32_t bucket_reqs,
                           int32_t block_width, void *hip_stream);
+
+/*
+ * The 8-bit KV cache.  It has the pages, the page table and the heads of the bf16
+ * cache, with e4m3 codes for cells and a scale for every token, KV head and kind
+ * (K or V): the row x of D values is stored as codes c = round(x / 2^e) (to
+ * nearest, ties to even; values that are not finite become NaN) with the least
+ * integer e >= -60 for which every finite |x_d| <= 448 * 2^e; it stands for c * 2^e,
+ * which bf16 holds exactly.
+ *   kv_pages   uint8 [num_pages][2][Hkv][16*D]; K tiles at [..][0][g], V at [..][1][g]:
+ *                K tile: element (slot s, dim d) at ((d/16)*16 + s)*16 + d%16
+ *                        (16-element d-chunks, slot-major inside a chunk);
+ *                V tile: element (slot s, dim d) at d*16 + s (d-major).
+ *              So a lane's 16-byte load is sixteen dims of one K row, or the sixteen
+ *              slots of one dim of V.
+ *   kv_scales  uint8 [num_pages][Hkv][2][16]: e + 127 of K ([..][0]) and V ([..][1])
+ *              by slot.
+ * Both must be 16-byte aligned.
+ *
+ * A cache slot is named by page * 16 + slot (the paper's "KV refs").
+ */
+
+/*
+ * Dimensions of one rope_append call.  All fields are host values.
+ *
+ *  rows           rows of q, k and v, >= 1.
+ *  num_q_heads    Hq >= 0 (0: no q; q and q_out are not used).
+ *  num_kv_heads   Hkv >= 1.
+ *  head_dim       D in {64, 128}.
+ *  page_size      must be DSV_PAGE_SIZE (16).
+ *  num_pages      pages of the cache, num_pages * 16 < 2^31.
+ *  in_dtype       DSV_BF16 or DSV_F32: of q, k and v.
+ *  kv_dtype       DSV_BF16 or DSV_FP8: of the cache.
+ *  rotary_dim     R, even, 0 <= R <= D: the first R dims of a head turn, the
+ *                 others pass.  0: nothing turns (positions and inv_freq unused).
+ *  interleaved    0: pair i is dims (i, i + R/2); 1: dims (2i, 2i + 1).
+ *  rope_scale     factor on the turned dims (1 unless a scaled method asks for
+ *                 another), finite.
+ *  q_stride, k_stride, v_stride
+ *                 elements from one row to the next (heads and dims are dense
+ *                 inside a row): >= heads * D, multiples of 8 (bf16) or 4 (fp32).
+ */
+typedef struct {
+  int32_t rows;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t num_pages;
+  int32_t in_dtype;
+  int32_t kv_dtype;
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float rope_scale;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+} dsv_append_dims;
+
+/*
+ * Rotary positions and the cache write of one step (or of a prompt).  For row r <
+ * live, pair i of every head of q and k turns by theta = positions[r] * inv_freq[i]:
+ *
+ *   (a, b) -> rope_scale * (a cos theta - b sin theta, b cos theta + a sin theta);
+ *
+ * q_out[r] is the turned q; the turned k and v[r] go to slot kv_refs[r] of the
+ * cache, the one that dsv_verify_attn, dsv_tree_attn and dsv_kv_read read.  A row
+ * whose kv_refs entry lies outside [0, num_pages * 16) is not written to the cache
+ * (its q is turned all the same).  Live rows must name distinct slots: one that two
+ * rows name holds a mixture.  Rows from live on, and slots that no row names, are
+ * left as they were.
+ *
+ *   q, k, v     bf16 or fp32 [rows][heads][D], rows `stride` elements apart (the
+ *               views of one projection's output serve as they are).
+ *   positions   int32 [rows].
+ *   inv_freq    fp32 [R/2]: radians to a position; scaled methods for long contexts
+ *               differ in these and in rope_scale only.
+ *   kv_refs     int32 [rows].
+ *   num_live    int32 scalar on the device, clamped into [0, rows] (cu_qlens + B of a
+ *               packed batch), or NULL: every row is live.
+ *   q_out       bf16 [rows][Hq][D]; may be q itself where that is dense bf16,
+ *               otherwise it must not overlap q, k or v.
+ *   kv_pages    bf16 (layout of dsv_verify_attn) or 8-bit codes; kv_scales for the
+ *               8-bit cache only (NULL otherwise).
+ * q, k, v, q_out, kv_pages and kv_scales must be 16-byte aligned.
+ * Precision: angles and k's rotation are in double precision, so the one rounding to
+ * bf16 or to a code is the exact value's (to 2^-50 of it); q is turned in fp32 and
+ * rounded once.  No workspace.
+ */
+int dsv_rope_append(const void *q, const void *k, const void *v, const int32_t *positions,
+                    const float *inv_freq, const int32_t *kv_refs, const int32_t *num_live,
+                    void *q_out, void *kv_pages, void *kv_scales,
+                    const dsv_append_dims *dims, void *hip_stream);
+
+/*
+ * Reads cache rows back: k_out[r], v_out[r] = the K and V rows of slot kv_refs[r], for
+ * r < rows; rows whose entry lies outside [0, num_pages * 16) are zeros.  A slot may
+ * be named any number of times.  Exact (an 8-bit cache's values fit bf16).
+ *   kv_pages, kv_scales  the bf16 (kv_dtype DSV_BF16, kv_scales NULL) or 8-bit cache.
+ *   k_out, v_out         bf16 or fp32 (out_dtype) [rows][Hkv][D].
+ * All but kv_refs must be 16-byte aligned.  rows >= 1, num_pages * 16 < 2^31.
+ */
+int dsv_kv_read(const void *kv_pages, const void *kv_scales, int32_t kv_dtype,
+                const int32_t *kv_refs, void *k_out, void *v_out, int32_t out_dtype,
+                int32_t rows, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                int32_t num_pages, void *hip_stream);
+
+/*
+ * A drafted tree.  Request i brings k_i = cu_qlens[i+1] - cu_qlens[i] nodes (0 for a
+ * sentinel, at most DSV_MAX_NODES), node 0 its root: the anchor.  Every other node
+ * comes after its parent.  Node n's token, logits and query sit in packed row
+ * cu_qlens[i] + n, and its K and V in cache position ctx_lens[i] + n, whatever its
+ * depth (its rotary position is ctx_lens[i] + depth).
+ *
+ * dsv_tree_masks makes, for every request, masks[cu_qlens[i] + n] = the bits of n and of
+ * its ancestors, and positions[cu_qlens[i] + n] = ctx_lens[i] + the number of its
+ * ancestors (positions may be NULL).
+ *   parents    int32 [capacity]: the parent's node number within the request; an entry
+ *              outside [0, n) makes node n a root of its own.
+ *   cu_qlens   int32 [B+1], as for dsv_verify_attn but k_i <= DSV_MAX_NODES.
+ *   masks      uint64 [capacity]; positions int32 [capacity].  Rows outside the
+ *              requests are left as they were.
+ * 1 <= num_reqs <= 65535, capacity >= 1.
+ */
+int dsv_tree_masks(const int32_t *parents, const int32_t *cu_qlens, const int32_t *ctx_lens,
+                   uint64_t *masks, int32_t *positions, int32_t num_reqs, int32_t capacity,
+                   void *hip_stream);
+
+/*
+ * Dimensions of one tree_attn call: as dsv_attn_dims, and
+ *  max_nodes   an upper bound on k_i over every call that uses the same dims, 1 ..
+ *              DSV_MAX_NODES; a request with more nodes is skipped.
+ *  kv_dtype    DSV_BF16 or DSV_FP8: of the cache.
+ */
+typedef struct {
+  int32_t num_reqs;
+  int32_t capacity;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t max_pages_per_req;
+  int32_t num_pages;
+  int32_t max_kv_len;
+  int32_t max_nodes;
+  int32_t kv_dtype;
+  float scale;
+} dsv_tree_dims;
+
+/* Workspace bytes dsv_tree_attn needs for `dims` (0 if dims are invalid): the work plan
+ * and fp32 partials, as for dsv_verify_attn_workspace_bytes. */
+size_t dsv_tree_attn_workspace_bytes(const dsv_tree_dims *dims);
+
+/*
+ * Attention of packed tree nodes over the paged cache.  Row cu_qlens[i] + j attends to
+ * keys t < ctx_lens[i] (the whole committed context) and to keys ctx_lens[i] + n of the
+ * nodes n < k_i whose bit is set in masks[cu_qlens[i] + j]:
+ *
+ *   out[row][h][:] = softmax_t( scale * q . K_t ) . V_t.
+ *
+ * A row that sees no key (ctx_lens[i] = 0 and an empty mask), or only keys whose
+ * score is minus infinity, is zeros.  Bits from k_i on are ignored.  A node that a row
+ * does not see has no part in it, also where its K or V hold infinities or NaN.
+ *   masks    uint64 [capacity] (of dsv_tree_masks, or any others), or NULL: row j sees
+ *            the nodes up to and including j (the causal block of dsv_verify_attn, for
+ *            blocks of up to 64 rows and for the 8-bit cache).
+ * Other arguments, layouts, tail rows and precision as for dsv_verify_attn; kv_pages and
+ * kv_scales as for dsv_rope_append.  Results are bitwise deterministic for given inputs.
+ */
+int dsv_tree_attn(const void *q_packed, const int32_t *cu_qlens, const uint64_t *masks,
+                  const void *kv_pages, const void *kv_scales, const int32_t *page_table,
+                  const int32_t *ctx_lens, void *out, const dsv_tree_dims *dims,
+                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Greedy acceptance of drafted trees.  With t_r = argmax_v logits_packed[r][v] as in
+ * dsv_accept, o = cu_qlens[i] and k = k_i, request i is walked from its root: from node
+ * c to its child n (parents[o+n] == c, n > c) with draft_tokens[o+n] == t_{o+c}, the
+ * lowest such n if there are several, until there is none.
+ *   accept_len[i]  the number of nodes accepted after the root (0 for a sentinel);
+ *   path[o + m]    the m-th node of the walk (path[o] = 0), m <= accept_len[i]; -1 in
+ *                  the request's other rows.  Rows outside the requests are left as they
+ *                  were;
+ *   next_token[i]  t of the last node (-1 for a sentinel).
+ * A chain (parents[o+n] = n - 1) gives dsv_accept's results.  Other arguments and the
+ * workspace (dsv_accept_workspace_bytes) as for dsv_accept; k_i <= DSV_MAX_NODES.
+ */
+int dsv_tree_accept(const void *logits_packed, int32_t dtype, const int32_t *cu_qlens,
+                    const int32_t *draft_tokens, const int32_t *parents, int32_t *accept_len,
+                    int32_t *path, int32_t *next_token, int32_t num_reqs, int32_t capacity,
+                    int32_t vocab, void *workspace, size_t workspace_bytes,
+                    void *hip_stream);
+
+/*
+ * Moves the accepted path of every request into place in one layer's cache: the K and V
+ * (and scales) of node path[o + m] go to position ctx_lens[i] + m, for m from 0 up to the
+ * path's first entry outside [0, k_i).  All of a request's rows are read before one is
+ * written.  The context of the next step is ctx_lens[i] + accept_len[i] + 1.  A row whose
+ * page ids lie outside [0, num_pages) is not moved; requests must not share the pages
+ * of their nodes.
+ *   kv_pages, kv_scales, kv_dtype, page_table [B][P_max], ctx_lens  as for dsv_tree_attn.
+ *   path, cu_qlens  as dsv_tree_accept leaves them.
+ * kv_pages must be 16-byte aligned.  1 <= num_reqs <= 65535, 1 <= num_kv_heads <= 65535.
+ */
+int dsv_tree_commit(void *kv_pages, void *kv_scales, int32_t kv_dtype,
+                    const int32_t *cu_qlens, const int32_t *ctx_lens,
+                    const int32_t *page_table, const int32_t *path, int32_t num_reqs,
+                    int32_t capacity, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t page_size, int32_t max_pages_per_req, int32_t num_pages,
+                    void *hip_stream);
 
 /*
  * Graph helpers for the fixed-address replay of Alg. 2 (capture once, replay

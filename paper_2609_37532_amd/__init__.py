@@ -13,6 +13,18 @@ and the decision step that produces their packed layout:
 * ``dvl_allocate_pack(...)`` -- DVL budget allocation and flat-buffer packing
   (verify lengths under the shared budget, the offsets, the packed rows).
 
+the paged cache's writer and reader, in bf16 or quantised to 8 bits,
+
+* ``rope_append(q, k, v, positions, inv_freq, kv_refs, q_out, kv_pages)`` -- rotary
+  positions (``rope_frequencies``) and the cache write of a step or a prompt;
+* ``kv_read(kv_pages, kv_refs, k_out, v_out)`` -- cache rows read back;
+
+and the verification of a drafted tree in place of a block:
+
+* ``tree_masks``, ``tree_attn``, ``tree_accept``, ``tree_commit`` -- masks and positions
+  from parents, attention over either cache, greedy acceptance, and the accepted path's
+  cache rows moved into place.
+
 ``BucketSet`` holds fixed-address buffers and the captured decision and
 verify graphs for a set of request-bucket sizes (``select_bucket``).
 
@@ -23,17 +35,21 @@ addresses; ``KernelTimer`` times the kernels with HIP events, and
 """
 from ._lib import (  # noqa: F401
     DSV_BF16,
+    DSV_FP8,
     DVL_MAX_REQS,
+    MAX_NODES,
     PRED_HIDDEN,
     DSV_F32,
     LIB_PATH,
     MAX_QLEN,
     PAGE_SIZE,
     TIMING_KINDS,
+    AppendDims,
     AttnDims,
     DSVError,
     Graph,
     KernelTimer,
+    TreeDims,
     accept,
     accept_noalloc,
     accept_stochastic,
@@ -44,9 +60,18 @@ from ._lib import (  # noqa: F401
     dvl_allocate_pack,
     predictor_forward,
     predictor_workspace_bytes,
+    kv_read,
     load,
     read_probe,
+    rope_append,
+    rope_frequencies,
     status_string,
+    tree_accept,
+    tree_attn,
+    tree_attn_dims,
+    tree_attn_workspace_bytes,
+    tree_commit,
+    tree_masks,
     validate_metadata,
     verify_attn,
     verify_attn_workspace_bytes,

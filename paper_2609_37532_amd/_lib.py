@@ -17,7 +17,9 @@ LIB_PATH = os.path.join(PKG, "libdsv.so")
 DSV_OK = 0
 DSV_F32 = 0
 DSV_BF16 = 1
+DSV_FP8 = 2
 MAX_QLEN = 16
+MAX_NODES = 64
 PAGE_SIZE = 16
 TIMING_KINDS = ("attn_split", "attn_combine", "accept_argmax", "accept_prefix", "dvl",
                 "sample_stats", "sample_draw", "predictor")
@@ -41,6 +43,23 @@ class AttnDims(ctypes.Structure):
 
     def as_dict(self) -> dict:
         return {f: getattr(self, f) for f, _ in self._fields_}
+
+
+class AppendDims(ctypes.Structure):
+    """Mirror of ``dsv_append_dims``."""
+    _fields_ = [(f, ctypes.c_int32) for f in (
+        "rows", "num_q_heads", "num_kv_heads", "head_dim", "page_size", "num_pages", "in_dtype",
+        "kv_dtype", "rotary_dim", "interleaved")] + [
+        ("rope_scale", ctypes.c_float)] + [(f, ctypes.c_int64) for f in (
+            "q_stride", "k_stride", "v_stride")]
+
+
+class TreeDims(ctypes.Structure):
+    """Mirror of ``dsv_tree_dims``."""
+    _fields_ = [(f, ctypes.c_int32) for f in (
+        "num_reqs", "capacity", "num_q_heads", "num_kv_heads", "head_dim", "page_size",
+        "max_pages_per_req", "num_pages", "max_kv_len", "max_nodes", "kv_dtype")] + [
+        ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -71,6 +90,13 @@ def load():
         "dsv_predictor_forward": (ctypes.c_int, [P, P, P, P, P, P, P, I32, I32, I32, I32, P,
                                                  SZ, P]),
         "dsv_dvl_allocate_pack": (ctypes.c_int, [P, P, P, P, P, P, P, P, P, P, P, I32, I32, P]),
+        "dsv_rope_append": (ctypes.c_int, [P] * 10 + [ctypes.POINTER(AppendDims), P]),
+        "dsv_kv_read": (ctypes.c_int, [P, P, I32, P, P, P, I32, I32, I32, I32, I32, I32, P]),
+        "dsv_tree_masks": (ctypes.c_int, [P, P, P, P, P, I32, I32, P]),
+        "dsv_tree_attn_workspace_bytes": (SZ, [ctypes.POINTER(TreeDims)]),
+        "dsv_tree_attn": (ctypes.c_int, [P] * 8 + [ctypes.POINTER(TreeDims), P, SZ, P]),
+        "dsv_tree_accept": (ctypes.c_int, [P, I32, P, P, P, P, P, P, I32, I32, I32, P, SZ, P]),
+        "dsv_tree_commit": (ctypes.c_int, [P, P, I32, P, P, P, P] + [I32] * 7 + [P]),
         "dsv_graph_capture_begin": (ctypes.c_int, [P]),
         "dsv_graph_capture_end": (ctypes.c_int, [P, ctypes.POINTER(ctypes.c_void_p)]),
         "dsv_graph_replay": (ctypes.c_int, [P, P]),
@@ -342,6 +368,278 @@ def dvl_allocate_pack(pred_logits, num_live, tokens, positions, kv_refs, k_out, 
         _ptr(k_out), _ptr(cu_qlens), _ptr(packed_tokens), _ptr(packed_positions),
         _ptr(packed_kv_refs), _ptr(scores_out), n_bs, w, _stream_handle(stream)))
 
+
+# ------------------------------------------------- cache rows and drafted trees
+def _require_here(*tensors) -> None:
+    """Every tensor on the current device: a stream of another one would run the
+    kernels there."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("tensors must be on the current device (cuda:%d), got %s"
+                             % (here, t.device))
+
+
+def _cache_dtype(kv_pages, kv_scales) -> int:
+    """Checks a cache's tensors; returns its ``kv_dtype``."""
+    import torch
+    if kv_scales is None:
+        _require(kv_pages, "kv_pages", _bf16_like(torch), 4)
+        dtype = DSV_BF16
+    else:
+        _require(kv_pages, "kv_pages", (torch.uint8, torch.float8_e4m3fn), 4)
+        _require(kv_scales, "kv_scales", (torch.uint8,), 4)
+        num_pages, _, hkv, _ = kv_pages.shape
+        if tuple(kv_scales.shape) != (num_pages, hkv, 2, PAGE_SIZE):
+            raise ValueError("kv_scales must be [P, Hkv, 2, 16]")
+        dtype = DSV_FP8
+    if kv_pages.shape[1] != 2 or kv_pages.shape[3] % PAGE_SIZE:
+        raise ValueError("kv_pages must be [P, 2, Hkv, 16*D]")
+    return dtype
+
+
+def _require_rows(t, name: str, dtype, rows: int, dim: int) -> int:
+    """Checks a [rows, heads, dim] tensor with dense heads; returns its row stride."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim:
+        raise ValueError("%s must be [%d, heads, %d]" % (name, rows, dim))
+    heads = t.shape[1]
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError("%s must have dense heads" % name)
+    return t.stride(0) if rows > 1 else heads * dim
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: Optional[str] = None,
+                     factor: float = 1.0, original_len: int = 0, beta_fast: float = 32.0,
+                     beta_slow: float = 1.0, device=None):
+    """``(inv_freq, rope_scale)`` for ``rope_append``: float32 [rotary_dim/2] on the
+    device, base ** (-2i / rotary_dim), and the factor on cos and sin.
+
+    ``scaling`` stretches a model's positions by ``factor``: ``"linear"`` divides every
+    frequency by it; ``"ntk"`` raises the base by factor ** (R / (R - 2)), which leaves the
+    fastest frequency and divides the slowest by it; ``"yarn"`` divides the frequencies
+    that make at most ``beta_slow`` turns within ``original_len`` positions, keeps those
+    that make ``beta_fast`` or more, blends linearly in the pair's index between, and
+    scales by 0.1 ln(factor) + 1."""
+    import torch
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim must be even and positive")
+    if not (base > 1 and factor >= 1):
+        raise ValueError("base must be above 1 and factor at least 1")
+    half = rotary_dim // 2
+    i = torch.arange(half, dtype=torch.float64)
+    scale = 1.0
+    if scaling == "ntk":
+        if half < 2:
+            raise ValueError("ntk scaling needs rotary_dim of at least 4")
+        base = base * factor ** (half / (half - 1))
+    inv = base ** (-i / half)
+    if scaling == "linear":
+        inv = inv / factor
+    elif scaling == "yarn":
+        if original_len < 1 or not beta_fast > beta_slow > 0:
+            raise ValueError("yarn scaling needs original_len and beta_fast > beta_slow > 0")
+        # the pair index whose frequency makes `turns` turns within original_len
+        at = lambda turns: half * math.log(original_len / (2 * math.pi * turns)) / math.log(base)
+        low = min(max(math.floor(at(beta_fast)), 0), half - 1)
+        high = min(max(math.ceil(at(beta_slow)), 0), half - 1)
+        slow = ((i - low) / max(high - low, 1e-3)).clamp(0, 1)
+        inv = inv * (1 - slow) + inv / factor * slow
+        scale = 0.1 * math.log(factor) + 1.0
+    elif scaling not in (None, "ntk"):
+        raise ValueError("scaling must be None, 'linear', 'ntk' or 'yarn'")
+    dev = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+    return inv.float().to(dev), scale
+
+
+def rope_append(q, k, v, positions, inv_freq, kv_refs, q_out, kv_pages, kv_scales=None, *,
+                interleaved: bool = False, rope_scale: float = 1.0, num_live=None,
+                stream=None) -> None:
+    """Enqueue ``dsv_rope_append``: q [rows, Hq, D] (or None) and k, v [rows, Hkv, D],
+    bf16 or float32, rows at any 16-byte aligned stride (views of one projection); q_out
+    bf16 [rows, Hq, D].  ``inv_freq`` None turns nothing.  ``kv_pages`` bf16, or uint8 with
+    ``kv_scales``; ``num_live`` int32 [1] on the device, or None."""
+    import torch
+    kv_dtype = _cache_dtype(kv_pages, kv_scales)
+    _require(kv_refs, "kv_refs", (torch.int32,), 1)
+    if k.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("k has dtype %s, expected bfloat16 or float32" % k.dtype)
+    rows, dim = kv_refs.shape[0], kv_pages.shape[3] // PAGE_SIZE
+    hkv = kv_pages.shape[2]
+    ks = _require_rows(k, "k", k.dtype, rows, dim)
+    vs = _require_rows(v, "v", k.dtype, rows, dim)
+    if k.shape[1] != hkv or v.shape[1] != hkv:
+        raise ValueError("k and v must have the cache's %d heads" % hkv)
+    hq = qs = 0
+    if q is not None:
+        qs = _require_rows(q, "q", k.dtype, rows, dim)
+        hq = q.shape[1]
+        _require(q_out, "q_out", (torch.bfloat16,), 3)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    rot = 0
+    if inv_freq is not None:
+        _require(inv_freq, "inv_freq", (torch.float32,), 1)
+        _require(positions, "positions", (torch.int32,), 1)
+        if positions.shape[0] != rows:
+            raise ValueError("positions must have %d entries" % rows)
+        rot = 2 * inv_freq.shape[0]
+    if num_live is not None:
+        _require(num_live, "num_live", (torch.int32,), 1)
+        if num_live.shape[0] != 1:
+            raise ValueError("num_live must hold one int32")
+    _require_here(q, k, v, q_out, kv_refs, kv_pages, kv_scales, positions, inv_freq, num_live)
+    dims = AppendDims(rows, hq, hkv, dim, PAGE_SIZE, kv_pages.shape[0],
+                      DSV_BF16 if k.dtype == torch.bfloat16 else DSV_F32, kv_dtype, rot,
+                      1 if interleaved else 0, float(rope_scale), qs, ks, vs)
+    _check("dsv_rope_append", load().dsv_rope_append(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(inv_freq), _ptr(kv_refs),
+        _ptr(num_live), _ptr(q_out), _ptr(kv_pages), _ptr(kv_scales), ctypes.byref(dims),
+        _stream_handle(stream)))
+
+
+def kv_read(kv_pages, kv_refs, k_out, v_out, kv_scales=None, *, stream=None) -> None:
+    """Enqueue ``dsv_kv_read``: the cache rows of the slots ``kv_refs`` (int32 [rows]) into
+    k_out, v_out [rows, Hkv, D], bf16 or float32."""
+    import torch
+    kv_dtype = _cache_dtype(kv_pages, kv_scales)
+    _require(kv_refs, "kv_refs", (torch.int32,), 1)
+    _require(k_out, "k_out", (torch.bfloat16, torch.float32), 3)
+    _require(v_out, "v_out", (k_out.dtype,), 3)
+    num_pages, _, hkv, tile = kv_pages.shape
+    want = (kv_refs.shape[0], hkv, tile // PAGE_SIZE)
+    if tuple(k_out.shape) != want or tuple(v_out.shape) != want:
+        raise ValueError("k_out and v_out must be [%d, %d, %d]" % want)
+    _require_here(kv_pages, kv_refs, k_out, v_out, kv_scales)
+    _check("dsv_kv_read", load().dsv_kv_read(
+        _ptr(kv_pages), _ptr(kv_scales), kv_dtype, _ptr(kv_refs), _ptr(k_out), _ptr(v_out),
+        DSV_BF16 if k_out.dtype == torch.bfloat16 else DSV_F32, want[0], hkv, want[2], PAGE_SIZE,
+        num_pages, _stream_handle(stream)))
+
+
+def tree_masks(parents, cu_qlens, ctx_lens, masks, positions=None, *, stream=None) -> None:
+    """Enqueue ``dsv_tree_masks``: ``parents`` int32 [cap] to ``masks`` int64 [cap] (the
+    bits of each node and its ancestors) and ``positions`` int32 [cap] or None."""
+    import torch
+    for t, n in ((parents, "parents"), (cu_qlens, "cu_qlens"), (ctx_lens, "ctx_lens")):
+        _require(t, n, (torch.int32,), 1)
+    _require(masks, "masks", (torch.int64, torch.uint64), 1)
+    cap, B = parents.shape[0], ctx_lens.shape[0]
+    if positions is not None:
+        _require(positions, "positions", (torch.int32,), 1)
+        if positions.shape[0] != cap:
+            raise ValueError("positions must be [cap]")
+    if masks.shape[0] != cap or cu_qlens.shape[0] != B + 1:
+        raise ValueError("masks must be [cap], cu_qlens [B+1] and ctx_lens [B]")
+    _require_here(parents, cu_qlens, ctx_lens, masks, positions)
+    _check("dsv_tree_masks", load().dsv_tree_masks(
+        _ptr(parents), _ptr(cu_qlens), _ptr(ctx_lens), _ptr(masks), _ptr(positions), B, cap,
+        _stream_handle(stream)))
+
+
+def tree_attn_dims(q_packed, kv_pages, page_table, kv_scales=None, *, max_nodes: int = MAX_NODES,
+                   max_kv_len: Optional[int] = None, scale: Optional[float] = None) -> TreeDims:
+    """``dsv_tree_dims`` from tensor shapes, as ``attn_dims``."""
+    a = attn_dims(q_packed, kv_pages, page_table, max_kv_len=max_kv_len, scale=scale)
+    return TreeDims(a.num_reqs, a.capacity, a.num_q_heads, a.num_kv_heads, a.head_dim,
+                    a.page_size, a.max_pages_per_req, a.num_pages, a.max_kv_len, max_nodes,
+                    DSV_BF16 if kv_scales is None else DSV_FP8, a.scale)
+
+
+def tree_attn_workspace_bytes(dims: TreeDims) -> int:
+    return int(load().dsv_tree_attn_workspace_bytes(ctypes.byref(dims)))
+
+
+def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv_scales=None, *,
+              max_nodes: int = MAX_NODES, max_kv_len: Optional[int] = None,
+              scale: Optional[float] = None, workspace=None, stream=None,
+              dims: Optional[TreeDims] = None) -> None:
+    """Enqueue ``dsv_tree_attn``: q_packed, out bf16 [cap, Hq, D]; ``masks`` int64 [cap]
+    (of ``tree_masks``) or None (causal); ``kv_pages`` bf16, or uint8 with ``kv_scales``."""
+    import torch
+    bf = _bf16_like(torch)
+    kv_dtype = _cache_dtype(kv_pages, kv_scales)
+    _require(q_packed, "q_packed", bf, 3)
+    _require(out, "out", bf, 3)
+    _require(cu_qlens, "cu_qlens", (torch.int32,), 1)
+    _require(page_table, "page_table", (torch.int32,), 2)
+    _require(ctx_lens, "ctx_lens", (torch.int32,), 1)
+    if dims is None:
+        dims = tree_attn_dims(q_packed, kv_pages, page_table, kv_scales, max_nodes=max_nodes,
+                              max_kv_len=max_kv_len, scale=scale)
+    cap, hq, dim = q_packed.shape
+    # dims made for other tensors would reach past these
+    if (dims.capacity, dims.num_q_heads, dims.head_dim) != (cap, hq, dim) or \
+            (dims.num_pages, dims.num_kv_heads) != (kv_pages.shape[0], kv_pages.shape[2]) or \
+            kv_pages.shape[3] != PAGE_SIZE * dim or dims.kv_dtype != kv_dtype or \
+            (dims.num_reqs, dims.max_pages_per_req) != tuple(page_table.shape):
+        raise ValueError("dims do not belong to these tensors")
+    if out.shape != q_packed.shape:
+        raise ValueError("out must have the shape of q_packed")
+    B = dims.num_reqs
+    if cu_qlens.shape[0] != B + 1 or ctx_lens.shape[0] != B:
+        raise ValueError("cu_qlens must have B+1 entries and ctx_lens B")
+    if masks is not None:
+        _require(masks, "masks", (torch.int64, torch.uint64), 1)
+        if masks.shape[0] != cap:
+            raise ValueError("masks must be [cap]")
+    if workspace is None:
+        workspace = alloc_workspace(tree_attn_workspace_bytes(dims), q_packed.device)
+    _require_here(q_packed, cu_qlens, masks, kv_pages, kv_scales, page_table, ctx_lens, out,
+                  workspace)
+    _check("dsv_tree_attn", load().dsv_tree_attn(
+        _ptr(q_packed), _ptr(cu_qlens), _ptr(masks), _ptr(kv_pages), _ptr(kv_scales),
+        _ptr(page_table), _ptr(ctx_lens), _ptr(out), ctypes.byref(dims), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path, next_token, *,
+                workspace=None, stream=None) -> None:
+    """Enqueue ``dsv_tree_accept``; logits float32 or bfloat16 [cap, vocab], ``parents`` and
+    ``path`` int32 [cap]; the workspace is ``accept``'s."""
+    import torch
+    _require(logits_packed, "logits_packed", (torch.float32, torch.bfloat16), 2)
+    cap, vocab = logits_packed.shape
+    B = cu_qlens.numel() - 1
+    for t, n, size in ((cu_qlens, "cu_qlens", B + 1), (draft_tokens, "draft_tokens", cap),
+                       (parents, "parents", cap), (accept_len, "accept_len", B),
+                       (path, "path", cap), (next_token, "next_token", B)):
+        _require(t, n, (torch.int32,), 1)
+        if t.shape[0] != size:
+            raise ValueError("%s must have %d entries" % (n, size))
+    if workspace is None:
+        workspace = alloc_workspace(accept_workspace_bytes(cap, B, vocab), logits_packed.device)
+    _require_here(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path, next_token,
+                  workspace)
+    _check("dsv_tree_accept", load().dsv_tree_accept(
+        _ptr(logits_packed), DSV_BF16 if logits_packed.dtype == torch.bfloat16 else DSV_F32,
+        _ptr(cu_qlens), _ptr(draft_tokens), _ptr(parents), _ptr(accept_len), _ptr(path),
+        _ptr(next_token), B, cap, vocab, _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+def tree_commit(kv_pages, cu_qlens, ctx_lens, page_table, path, kv_scales=None, *,
+                stream=None) -> None:
+    """Enqueue ``dsv_tree_commit``: the accepted path's cache rows of one layer, moved to
+    the positions after the context."""
+    import torch
+    kv_dtype = _cache_dtype(kv_pages, kv_scales)
+    for t, n in ((cu_qlens, "cu_qlens"), (ctx_lens, "ctx_lens"), (path, "path")):
+        _require(t, n, (torch.int32,), 1)
+    _require(page_table, "page_table", (torch.int32,), 2)
+    num_pages, _, hkv, tile = kv_pages.shape
+    B, pmax = page_table.shape
+    if cu_qlens.shape[0] != B + 1 or ctx_lens.shape[0] != B:
+        raise ValueError("cu_qlens must have B+1 entries and ctx_lens B")
+    _require_here(kv_pages, cu_qlens, ctx_lens, page_table, path, kv_scales)
+    _check("dsv_tree_commit", load().dsv_tree_commit(
+        _ptr(kv_pages), _ptr(kv_scales), kv_dtype, _ptr(cu_qlens), _ptr(ctx_lens),
+        _ptr(page_table), _ptr(path), B, path.shape[0], hkv, tile // PAGE_SIZE, PAGE_SIZE, pmax,
+        num_pages, _stream_handle(stream)))
 
 
 PROBE_TILE_BYTES = 4096

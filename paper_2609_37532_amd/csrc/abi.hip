@@ -40,6 +40,48 @@ int check_dims(const dsv_attn_dims *d) {
   return DSV_OK;
 }
 
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Head dim, page size and page count of a cache that slots are named in.
+int check_cache(int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
+                int32_t kv_dtype) {
+  if (num_kv_heads < 1 || num_kv_heads > 65535 || num_pages < 1 ||
+      num_pages > INT32_MAX / DSV_PAGE_SIZE)
+    return DSV_ERR_DIMS;
+  if (page_size != DSV_PAGE_SIZE) return DSV_ERR_UNSUPPORTED;
+  if (head_dim != 64 && head_dim != 128) return DSV_ERR_UNSUPPORTED;
+  if (kv_dtype != DSV_BF16 && kv_dtype != DSV_FP8) return DSV_ERR_UNSUPPORTED;
+  return DSV_OK;
+}
+
+// An 8-bit cache has scales, a bf16 one none.
+int check_pages(const void *pages, const void *scales, int32_t kv_dtype) {
+  if (!pages || (kv_dtype == DSV_FP8 && !scales)) return DSV_ERR_NULL;
+  if (kv_dtype == DSV_BF16 && scales) return DSV_ERR_UNSUPPORTED;
+  if (!aligned16(pages) || !aligned16(scales)) return DSV_ERR_UNSUPPORTED;
+  return DSV_OK;
+}
+
+int check_tree_dims(const dsv_tree_dims *d) {
+  if (!d) return DSV_ERR_NULL;
+  const dsv_attn_dims same = {d->num_reqs,          d->capacity,  d->num_q_heads, d->num_kv_heads,
+                              d->head_dim,          d->page_size, d->max_pages_per_req,
+                              d->num_pages,         d->max_kv_len, d->scale};
+  const int rc = check_dims(&same);
+  if (rc != DSV_OK) return rc;
+  if (d->max_nodes < 1 || d->max_nodes > DSV_MAX_NODES) return DSV_ERR_DIMS;
+  if (d->kv_dtype != DSV_BF16 && d->kv_dtype != DSV_FP8) return DSV_ERR_UNSUPPORTED;
+  // the flattened work counts every row group of a KV head as a segment
+  const long long groups = tree_workspace_layout(*d).row_groups;
+  const long long seg_keys =
+      (long long)(d->max_kv_len + kAttnBlockKeys - 1) / kAttnBlockKeys * kAttnBlockKeys +
+      kAttnLeadKeys;
+  if (d->num_kv_heads * groups > 65535 ||
+      d->num_kv_heads * groups * d->num_reqs * seg_keys >= (1LL << 30))
+    return DSV_ERR_DIMS;
+  return DSV_OK;
+}
+
 __global__ void validate_kernel(const int32_t *cu, const int32_t *ctx,
                                 const int32_t *page_table, dsv_attn_dims d,
                                 int32_t *err_word) {
@@ -437,6 +479,186 @@ int dsv_dvl_allocate_pack(const float *pred_logits, const int32_t *num_live,
                                   k_out, cu_qlens, packed_tokens, packed_positions,
                                   packed_kv_refs, scores_out, bucket_reqs, block_width,
                                   (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+int dsv_rope_append(const void *q, const void *k, const void *v, const int32_t *positions,
+                    const float *inv_freq, const int32_t *kv_refs, const int32_t *num_live,
+                    void *q_out, void *kv_pages, void *kv_scales,
+                    const dsv_append_dims *dims, void *hip_stream) {
+  if (!dims || !k || !v || !kv_refs) return DSV_ERR_NULL;
+  const dsv_append_dims &d = *dims;
+  int rc = check_cache(d.num_kv_heads, d.head_dim, d.page_size, d.num_pages, d.kv_dtype);
+  if (rc != DSV_OK) return rc;
+  if (d.rows < 1 || d.rows > (1 << 24) || d.num_q_heads < 0 || d.num_q_heads > 65535 ||
+      d.rotary_dim < 0 || d.rotary_dim > d.head_dim || d.rotary_dim % 2 != 0 ||
+      (d.interleaved != 0 && d.interleaved != 1) || !isfinite(d.rope_scale) ||
+      (long long)d.rows * d.num_kv_heads > (1LL << 30))
+    return DSV_ERR_DIMS;
+  if (d.in_dtype != DSV_BF16 && d.in_dtype != DSV_F32) return DSV_ERR_UNSUPPORTED;
+  if ((d.num_q_heads > 0 && (!q || !q_out)) || (d.rotary_dim > 0 && (!positions || !inv_freq)))
+    return DSV_ERR_NULL;
+  rc = check_pages(kv_pages, kv_scales, d.kv_dtype);
+  if (rc != DSV_OK) return rc;
+  const int64_t q_row = (int64_t)d.num_q_heads * d.head_dim;
+  const int64_t kv_row = (int64_t)d.num_kv_heads * d.head_dim;
+  constexpr int64_t kMost = (int64_t)1 << 40;  // row offsets stay far inside 64 bits
+  if ((d.num_q_heads > 0 && (d.q_stride < q_row || d.q_stride > kMost)) || d.k_stride < kv_row ||
+      d.k_stride > kMost || d.v_stride < kv_row || d.v_stride > kMost)
+    return DSV_ERR_DIMS;
+  // rows move in 16-byte vectors
+  const int64_t vec = d.in_dtype == DSV_F32 ? 4 : 8;
+  if (!aligned16(k) || !aligned16(v) || d.k_stride % vec != 0 || d.v_stride % vec != 0)
+    return DSV_ERR_UNSUPPORTED;
+  if (d.num_q_heads > 0 && (!aligned16(q) || !aligned16(q_out) || d.q_stride % vec != 0))
+    return DSV_ERR_UNSUPPORTED;
+
+  AppendParams p = {};
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.pos = positions;
+  p.inv_freq = inv_freq;
+  p.refs = kv_refs;
+  p.num_live = num_live;
+  p.q_out = (uint16_t *)q_out;
+  p.pages = kv_pages;
+  p.scales = (uint8_t *)kv_scales;
+  p.q_stride = d.q_stride;
+  p.k_stride = d.k_stride;
+  p.v_stride = d.v_stride;
+  p.rows = d.rows;
+  p.hq = d.num_q_heads;
+  p.hkv = d.num_kv_heads;
+  p.rot = d.rotary_dim;
+  p.interleaved = d.interleaved;
+  p.num_pages = d.num_pages;
+  p.rope_scale = d.rope_scale;
+  const hipError_t e = launch_rope_append(p, d.head_dim, d.in_dtype == DSV_F32,
+                                          d.kv_dtype == DSV_FP8, (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+int dsv_kv_read(const void *kv_pages, const void *kv_scales, int32_t kv_dtype,
+                const int32_t *kv_refs, void *k_out, void *v_out, int32_t out_dtype,
+                int32_t rows, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                int32_t num_pages, void *hip_stream) {
+  if (!kv_refs || !k_out || !v_out) return DSV_ERR_NULL;
+  int rc = check_cache(num_kv_heads, head_dim, page_size, num_pages, kv_dtype);
+  if (rc != DSV_OK) return rc;
+  if (rows < 1 || rows > (1 << 30) || (long long)rows * num_kv_heads > (1LL << 33))
+    return DSV_ERR_DIMS;
+  if (out_dtype != DSV_BF16 && out_dtype != DSV_F32) return DSV_ERR_UNSUPPORTED;
+  rc = check_pages(kv_pages, kv_scales, kv_dtype);
+  if (rc != DSV_OK) return rc;
+  if (!aligned16(k_out) || !aligned16(v_out)) return DSV_ERR_UNSUPPORTED;
+  const ReadParams p = {kv_pages, (const uint8_t *)kv_scales, kv_refs, k_out, v_out,
+                        rows,     num_kv_heads,               num_pages};
+  const hipError_t e = launch_kv_read(p, head_dim, kv_dtype == DSV_FP8, out_dtype == DSV_F32,
+                                      (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+int dsv_tree_masks(const int32_t *parents, const int32_t *cu_qlens, const int32_t *ctx_lens,
+                   uint64_t *masks, int32_t *positions, int32_t num_reqs, int32_t capacity,
+                   void *hip_stream) {
+  if (!parents || !cu_qlens || !ctx_lens || !masks) return DSV_ERR_NULL;
+  if (num_reqs < 1 || num_reqs > 65535 || capacity < 1) return DSV_ERR_DIMS;
+  const hipError_t e =
+      launch_tree_masks(parents, cu_qlens, ctx_lens, (unsigned long long *)masks, positions,
+                        num_reqs, capacity, (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+size_t dsv_tree_attn_workspace_bytes(const dsv_tree_dims *dims) {
+  if (check_tree_dims(dims) != DSV_OK) return 0;
+  return tree_workspace_layout(*dims).total;
+}
+
+int dsv_tree_attn(const void *q_packed, const int32_t *cu_qlens, const uint64_t *masks,
+                  const void *kv_pages, const void *kv_scales, const int32_t *page_table,
+                  const int32_t *ctx_lens, void *out, const dsv_tree_dims *dims,
+                  void *workspace, size_t workspace_bytes, void *hip_stream) {
+  if (!q_packed || !cu_qlens || !page_table || !ctx_lens || !out) return DSV_ERR_NULL;
+  int rc = check_tree_dims(dims);
+  if (rc != DSV_OK) return rc;
+  rc = check_pages(kv_pages, kv_scales, dims->kv_dtype);
+  if (rc != DSV_OK) return rc;
+  if (!aligned16(q_packed) || !aligned16(out)) return DSV_ERR_UNSUPPORTED;
+  const TreeWorkspace ws = tree_workspace_layout(*dims);
+  if (!workspace || !aligned256(workspace) || workspace_bytes < ws.total)
+    return DSV_ERR_WORKSPACE;
+  const int32_t grid = tree_grid(*dims);
+  if (grid <= 0) return DSV_ERR_HIP;  // device query failed
+
+  TreeParams p;
+  p.q = (const uint16_t *)q_packed;
+  p.cu = cu_qlens;
+  p.masks = (const unsigned long long *)masks;
+  p.kv = kv_pages;
+  p.scales = (const uint8_t *)kv_scales;
+  p.page_table = page_table;
+  p.ctx = ctx_lens;
+  p.out = (uint16_t *)out;
+  p.plan = (int32_t *)((char *)workspace + ws.plan_off);
+  p.part_ml = (float2 *)((char *)workspace + ws.part_ml_off);
+  p.part_o = (float *)((char *)workspace + ws.part_o_off);
+  p.num_reqs = dims->num_reqs;
+  p.cap = dims->capacity;
+  p.hq = dims->num_q_heads;
+  p.hkv = dims->num_kv_heads;
+  p.group = dims->num_q_heads / dims->num_kv_heads;
+  p.max_pages = dims->max_pages_per_req;
+  p.num_pages = dims->num_pages;
+  p.max_kv_len = dims->max_kv_len;
+  p.max_nodes = dims->max_nodes;
+  p.group_rows = ws.group_rows;
+  p.num_cu = attn_num_cu();
+  p.scale_log2 = dims->scale * 1.4426950408889634f;
+  const hipError_t e = launch_tree_attn(p, *dims, grid, (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+int dsv_tree_accept(const void *logits_packed, int32_t dtype, const int32_t *cu_qlens,
+                    const int32_t *draft_tokens, const int32_t *parents, int32_t *accept_len,
+                    int32_t *path, int32_t *next_token, int32_t num_reqs, int32_t capacity,
+                    int32_t vocab, void *workspace, size_t workspace_bytes,
+                    void *hip_stream) {
+  if (!logits_packed || !cu_qlens || !draft_tokens || !parents || !accept_len || !path ||
+      !next_token)
+    return DSV_ERR_NULL;
+  if (num_reqs < 1 || capacity < 1 || vocab < 1 || capacity > 65535 ||
+      num_reqs > (1 << 30))
+    return DSV_ERR_DIMS;
+  if (dtype != DSV_F32 && dtype != DSV_BF16) return DSV_ERR_UNSUPPORTED;
+  const AcceptWorkspace ws = accept_workspace_layout(capacity, vocab);
+  if (!workspace || !aligned256(workspace) || workspace_bytes < ws.total)
+    return DSV_ERR_WORKSPACE;
+  const hipError_t e = launch_tree_accept(
+      logits_packed, dtype, cu_qlens, draft_tokens, parents, accept_len, path, next_token,
+      num_reqs, capacity, vocab, (float *)((char *)workspace + ws.val_off),
+      (int32_t *)((char *)workspace + ws.idx_off), ws.num_chunks, (hipStream_t)hip_stream);
+  return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
+}
+
+int dsv_tree_commit(void *kv_pages, void *kv_scales, int32_t kv_dtype,
+                    const int32_t *cu_qlens, const int32_t *ctx_lens,
+                    const int32_t *page_table, const int32_t *path, int32_t num_reqs,
+                    int32_t capacity, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t page_size, int32_t max_pages_per_req, int32_t num_pages,
+                    void *hip_stream) {
+  if (!cu_qlens || !ctx_lens || !page_table || !path) return DSV_ERR_NULL;
+  int rc = check_cache(num_kv_heads, head_dim, page_size, num_pages, kv_dtype);
+  if (rc != DSV_OK) return rc;
+  if (num_reqs < 1 || num_reqs > 65535 || capacity < 1 || max_pages_per_req < 1)
+    return DSV_ERR_DIMS;
+  rc = check_pages(kv_pages, kv_scales, kv_dtype);
+  if (rc != DSV_OK) return rc;
+  const CommitParams p = {kv_pages, (uint8_t *)kv_scales, cu_qlens, ctx_lens, page_table,
+                          path,     num_kv_heads,         capacity, max_pages_per_req,
+                          num_pages};
+  const hipError_t e = launch_tree_commit(p, num_reqs, head_dim, kv_dtype == DSV_FP8,
+                                          (hipStream_t)hip_stream);
   return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;
 }
 

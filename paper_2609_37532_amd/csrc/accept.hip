@@ -16,6 +16,9 @@
 // order and does the prefix compare with a ballot.  The comparison is exact
 // (bf16 and fp32 widen exactly to fp32), so the result is bit-exact and
 // independent of scheduling.
+//
+// A tree of drafted tokens takes the same argmax, then a walk from its root in place
+// of the prefix compare.
 #include "dsv_internal.h"
 
 #include <math.h>
@@ -171,6 +174,30 @@ __global__ __launch_bounds__(kThreads) void argmax_chunk_kernel(
   }
 }
 
+// Argmax of a row: its chunk pairs in chunk order, loaded kBatch at a time so that the
+// loads of a batch are in flight together (one batch up to 32 chunks, a 262,144-token
+// vocabulary).
+__device__ __forceinline__ int row_choice(const float *best_val, const int32_t *best_idx,
+                                          int row, int num_chunks) {
+  constexpr int kBatch = 32;
+  const size_t base = (size_t)row * num_chunks;
+  float bv = -INFINITY;
+  int bi = 0x7FFFFFFF;
+  for (int c0 = 0; c0 < num_chunks; c0 += kBatch) {
+    float v[kBatch];
+    int x[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int c = min(c0 + u, num_chunks - 1);  // clamped: repeats are harmless
+      v[u] = best_val[base + c];
+      x[u] = best_idx[base + c];
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) take(bv, bi, v[u], x[u]);
+  }
+  return bi;
+}
+
 // One wave per request: lane j reduces row o+j over the chunks (in chunk
 // order), the ballot of mismatches gives the accepted length.
 __global__ __launch_bounds__(kWave) void prefix_kernel(
@@ -190,28 +217,7 @@ __global__ __launch_bounds__(kWave) void prefix_kernel(
   // the drafted token each row is compared with, loaded with the chunk pairs
   const int want = lane < k - 1 ? draft[o + lane + 1] : -1;
   int t = -1;
-  if (lane < k) {
-    // the row's chunk pairs in chunk order, loaded kBatch at a time so that
-    // the loads of a batch are in flight together (one batch up to 32
-    // chunks, a 262,144-token vocabulary)
-    constexpr int kBatch = 32;
-    const size_t base = (size_t)(o + lane) * num_chunks;
-    float bv = -INFINITY;
-    int bi = 0x7FFFFFFF;
-    for (int c0 = 0; c0 < num_chunks; c0 += kBatch) {
-      float v[kBatch];
-      int x[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int c = min(c0 + u, num_chunks - 1);  // clamped: repeats are harmless
-        v[u] = best_val[base + c];
-        x[u] = best_idx[base + c];
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) take(bv, bi, v[u], x[u]);
-    }
-    t = bi;
-  }
+  if (lane < k) t = row_choice(best_val, best_idx, o + lane, num_chunks);
   const bool mismatch = lane < k - 1 && t != want;
   const unsigned long long mask = __ballot(mismatch);
   const int a = mask ? __builtin_ctzll(mask) : k - 1;
@@ -220,6 +226,58 @@ __global__ __launch_bounds__(kWave) void prefix_kernel(
     accept_len[i] = a;
     next_token[i] = succ;
   }
+}
+
+// The tree verifier, one wave per request: lane j is node j, with its row's choice, its
+// token and its parent.  From node 0 on, the lowest child of the current node whose
+// token is the node's choice is accepted; a child comes after its parent, so the walk
+// takes at most k - 1 steps, each a ballot.
+__global__ __launch_bounds__(kWave) void tree_walk_kernel(
+    const int32_t *cu, const int32_t *draft, const int32_t *parents, int32_t *accept_len,
+    int32_t *path, int32_t *next_token, int32_t cap, int32_t num_chunks, const float *best_val,
+    const int32_t *best_idx) {
+  const int i = blockIdx.x, lane = threadIdx.x;
+  const int o = cu[i], k = cu[i + 1] - o;
+  if (k == 0) {
+    if (lane == 0) {
+      accept_len[i] = 0;
+      next_token[i] = -1;
+    }
+    return;
+  }
+  if (k < 0 || k > kMaxNodes || o < 0 || o + k > cap) return;  // bad metadata
+  const int token = lane < k ? draft[o + lane] : -1;
+  int up = lane < k ? parents[o + lane] : -1;
+  if (up >= lane) up = -1;  // a parent comes before its node
+  const int t = lane < k ? row_choice(best_val, best_idx, o + lane, num_chunks) : -1;
+  int at = 0, len = 0, mine = lane == 0 ? 0 : -1;
+  for (;;) {
+    const int want = __builtin_amdgcn_readlane(t, at);
+    const unsigned long long next = __ballot(lane < k && up == at && token == want);
+    if (next == 0) break;
+    at = __builtin_ctzll(next);  // after the node it was reached from
+    ++len;
+    if (lane == len) mine = at;
+  }
+  const int succ = __builtin_amdgcn_readlane(t, at);
+  if (lane < k) path[o + lane] = mine;
+  if (lane == 0) {
+    accept_len[i] = len;
+    next_token[i] = succ;
+  }
+}
+
+// The argmax of every live row into the workspace's chunk pairs.
+void launch_argmax(const void *logits, int dtype, const int32_t *cu, int32_t num_reqs,
+                   int32_t cap, int32_t vocab, float *best_val, int32_t *best_idx,
+                   int32_t num_chunks, hipStream_t s) {
+  const dim3 grid(num_chunks, cap);
+  if (dtype == DSV_BF16)
+    launch_kernel(argmax_chunk_kernel<true>, grid, dim3(kThreads), s, logits, cu, num_reqs, cap,
+                  vocab, num_chunks, best_val, best_idx);
+  else
+    launch_kernel(argmax_chunk_kernel<false>, grid, dim3(kThreads), s, logits, cu, num_reqs,
+                  cap, vocab, num_chunks, best_val, best_idx);
 }
 
 }  // namespace
@@ -256,19 +314,25 @@ hipError_t launch_accept(const void *logits, int dtype, const int32_t *cu,
                          int32_t *next_token, int32_t num_reqs, int32_t cap,
                          int32_t vocab, float *best_val, int32_t *best_idx,
                          int32_t num_chunks, hipStream_t s) {
-  const dim3 grid(num_chunks, cap);
   timing_mark(kTimeArgmax, false, s);
-  if (dtype == DSV_BF16)
-    launch_kernel(argmax_chunk_kernel<true>, grid, dim3(kThreads), s, logits, cu, num_reqs, cap,
-                  vocab, num_chunks, best_val, best_idx);
-  else
-    launch_kernel(argmax_chunk_kernel<false>, grid, dim3(kThreads), s, logits, cu, num_reqs,
-                  cap, vocab, num_chunks, best_val, best_idx);
+  launch_argmax(logits, dtype, cu, num_reqs, cap, vocab, best_val, best_idx, num_chunks, s);
   timing_mark(kTimeArgmax, true, s);
   timing_mark(kTimePrefix, false, s);
   launch_kernel(prefix_kernel, dim3(num_reqs), dim3(kWave), s, cu, draft, accept_len,
                 next_token, num_reqs, cap, num_chunks, best_val, best_idx);
   timing_mark(kTimePrefix, true, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_accept(const void *logits, int dtype, const int32_t *cu,
+                              const int32_t *draft, const int32_t *parents,
+                              int32_t *accept_len, int32_t *path, int32_t *next_token,
+                              int32_t num_reqs, int32_t cap, int32_t vocab, float *best_val,
+                              int32_t *best_idx, int32_t num_chunks, hipStream_t s) {
+  launch_argmax(logits, dtype, cu, num_reqs, cap, vocab, best_val, best_idx, num_chunks, s);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  launch_kernel(tree_walk_kernel, dim3(num_reqs), dim3(kWave), s, cu, draft, parents, accept_len,
+                path, next_token, cap, num_chunks, best_val, best_idx);
   return hipGetLastError();
 }
 

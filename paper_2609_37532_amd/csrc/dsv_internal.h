@@ -116,6 +116,83 @@ hipError_t launch_dvl(const float *pred_logits, const int32_t *num_live,
                       int32_t *ptok, int32_t *ppos, int32_t *pref, float *scores,
                       int32_t n_bs, int32_t w, hipStream_t s);
 
+// -------------------------------------------------------------------------
+// cache rows: written with rotary positions, read back, moved
+// -------------------------------------------------------------------------
+constexpr int kMaxNodes = DSV_MAX_NODES;
+struct AppendParams {
+  const void *q, *k, *v;    // bf16 or fp32, row strides in elements
+  const int32_t *pos;       // [rows]
+  const float *inv_freq;    // [rot / 2]
+  const int32_t *refs;      // [rows]
+  const int32_t *num_live;  // or nullptr
+  uint16_t *q_out;          // bf16 [rows][Hq][D]
+  void *pages;              // [P][2][Hkv][16*D], bf16 or 8-bit codes
+  uint8_t *scales;          // [P][Hkv][2][16] (8-bit cache)
+  int64_t q_stride, k_stride, v_stride;
+  int32_t rows, hq, hkv, rot, interleaved, num_pages;
+  float rope_scale;
+  // set by the launcher: the pairs' form (PairMode in cache.hip), workgroups that write
+  // the cache, KV heads and rows of q to one
+  int32_t mode, kv_blocks, heads_per_block, q_rows;
+};
+hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipStream_t s);
+
+struct ReadParams {
+  const void *pages;
+  const uint8_t *scales;
+  const int32_t *refs;
+  void *k_out, *v_out;  // [rows][Hkv][D]
+  int32_t rows, hkv, num_pages;
+};
+hipError_t launch_kv_read(const ReadParams &p, int dim, bool fp8, bool f32, hipStream_t s);
+
+struct CommitParams {
+  void *pages;
+  uint8_t *scales;
+  const int32_t *cu, *ctx, *page_table, *path;
+  int32_t hkv, cap, max_pages, num_pages;
+};
+hipError_t launch_tree_commit(const CommitParams &p, int num_reqs, int dim, bool fp8,
+                              hipStream_t s);
+
+// -------------------------------------------------------------------------
+// trees of drafted tokens
+// -------------------------------------------------------------------------
+struct TreeParams {
+  const uint16_t *q;          // bf16 [cap][Hq][D]
+  const int32_t *cu;          // [B+1]
+  const unsigned long long *masks;  // [cap] or nullptr (causal)
+  const void *kv;             // [P][2][Hkv][16*D], bf16 or 8-bit codes
+  const uint8_t *scales;      // [P][Hkv][2][16] (8-bit cache)
+  const int32_t *page_table;  // [B][P_max]
+  const int32_t *ctx;         // [B]
+  uint16_t *out;              // bf16 [cap][Hq][D]
+  int32_t *plan;              // [2B+3], as for verify attention, in units of all segments
+  float2 *part_ml;            // fp32 [grid][2][rows] x (m, l)
+  float *part_o;              // fp32 [grid][2][rows][D]
+  int32_t num_reqs, cap, hq, hkv, group, max_pages, num_pages, max_kv_len, max_nodes;
+  int32_t group_rows;  // rows of a segment's partial: the most rows one workgroup holds
+  int32_t num_cu;
+  float scale_log2;
+};
+struct TreeWorkspace {
+  size_t plan_off, part_ml_off, part_o_off, total;
+  int32_t group_rows, row_groups;
+};
+TreeWorkspace tree_workspace_layout(const dsv_tree_dims &d);
+int32_t tree_grid(const dsv_tree_dims &d);  // launch grid on the current device
+hipError_t launch_tree_attn(const TreeParams &p, const dsv_tree_dims &d, int32_t grid,
+                            hipStream_t s);
+hipError_t launch_tree_masks(const int32_t *parents, const int32_t *cu, const int32_t *ctx,
+                             unsigned long long *masks, int32_t *positions, int32_t num_reqs,
+                             int32_t cap, hipStream_t s);
+hipError_t launch_tree_accept(const void *logits, int dtype, const int32_t *cu,
+                              const int32_t *draft, const int32_t *parents,
+                              int32_t *accept_len, int32_t *path, int32_t *next_token,
+                              int32_t num_reqs, int32_t cap, int32_t vocab, float *best_val,
+                              int32_t *best_idx, int32_t num_chunks, hipStream_t s);
+
 // Kernel kinds of the timing hook (see dsv_timing_start).
 enum TimingKind {
   kTimeAttnSplit = 0,

@@ -1,0 +1,926 @@
+// tree.hip -- attention of drafted trees over a paged GQA KV cache, bf16 or 8-bit
+// (gfx950), and the masks that a tree's parents stand for.
+//
+// What it computes: row j of request i (node j of its tree) attends to the committed
+// context, keys 0 .. ctx_i - 1, and to the nodes n whose bit is set in the row's mask,
+// keys ctx_i + n (without masks: n <= j, the causal block).  A row that sees no key is 0.
+//
+// How.  The key loop, the LDS ring and the arithmetic of the work split are verify
+// attention's (attn_core.h).  What differs:
+//  * A tree of 64 nodes under 16 query heads has 1,024 rows to a KV head, more than a
+//    workgroup's registers hold.  A request's rows are cut into row groups of up to
+//    `group_rows` rows, and a segment of the work is (request, KV head, row group); the
+//    groups of one KV head lie next to each other in the plan, so that the second one's
+//    K and V come out of the cache.
+//  * Masks only matter in the one to three blocks that hold nodes.  There each lane
+//    takes its row's 64-bit mask, shifted so that bit b is key t0 + b; other blocks are
+//    as in verify attention.
+//  * Nodes that a row does not see may hold anything, also infinities and NaN: a
+//    weight of 0 times such a V would be NaN in the matrix product.  Where a block of
+//    nodes holds one (a test of the block's V operands), its V cells that are not finite
+//    are taken out of the product and brought to the rows that see them by three
+//    products of ones and zeros.
+//  * An 8-bit cache is half the bytes.  Codes become bf16 on the way from the load
+//    registers to the LDS ring, their scale (a power of two) multiplied in, which is
+//    exact, so the ring and all after it are the bf16 cache's, and each code is converted
+//    once for all waves.
+#include "attn_core.h"
+
+#include <atomic>
+
+namespace dsv {
+namespace {
+
+constexpr int kCombThreads = 1024;  // as verify attention's combine
+
+// Request-level metadata after the device-side checks: seg is ctx + k rounded up to
+// whole blocks, 0 for a request without rows or with metadata out of range; groups its
+// row groups.
+struct TreeMeta {
+  int q0, k, ctx, len, seg, groups;
+};
+
+__device__ __forceinline__ TreeMeta tree_meta(const TreeParams &p, int q0, int q1, int ctx) {
+  TreeMeta r;
+  r.q0 = q0;
+  r.ctx = ctx;
+  r.k = q1 - q0;
+  const bool ok = q0 >= 0 && q1 <= p.cap && r.k > 0 && r.k <= p.max_nodes && ctx >= 0 &&
+                  ctx <= p.max_kv_len - r.k;
+  r.len = ok ? ctx + r.k : 0;
+  r.seg = round_up_block(r.len);
+  r.groups = ok ? (p.group * r.k + p.group_rows - 1) >> __builtin_ctz(p.group_rows) : 0;
+  return r;
+}
+__device__ __forceinline__ TreeMeta tree_meta(const TreeParams &p, int i) {
+  return tree_meta(p, p.cu[i], p.cu[i + 1], p.ctx[i]);
+}
+
+// A workgroup's share of the work, [start, end) in keys over all segments laid end to
+// end: request, then KV head, then row group.
+struct TreeShare {
+  int start, end;
+  int i, sub, off;  // request, segment of the request, virtual offset where `start` falls
+  int lead;         // keys of lead-in per segment: kLeadKeys (stream-K) or 0
+  TreeMeta first;
+};
+
+// The plan of verify attention (plan_share in attn.hip: stream-K shares, or equal pieces
+// of segments for small batches) over segments whose number differs by request.
+// Workgroup 0 publishes the prefixes for the combine kernel.  LDS use: scan totals, the
+// located share, the small-batch counts.
+template <int D, int NW>
+__device__ TreeShare tree_plan(const TreeParams &p, int *lds) {
+  constexpr int kThreads = NW * kWave;
+  const int B = p.num_reqs, tid = threadIdx.x;
+  int live = p.cu[B];
+  const int per = (B + kThreads - 1) / kThreads;
+  const int lo = min(B, tid * per), hi = min(B, lo + per);
+  TreeMeta mine = {};  // this thread's request where each has one
+  int work = 0, segs = 0;
+  for (int i = lo; i < hi; ++i) {
+    mine = tree_meta(p, i);
+    segs += mine.groups * p.hkv;
+    work += mine.groups * p.hkv * mine.seg;
+  }
+  asm volatile("" : "+v"(live));  // its load is in flight with the others
+  auto meta = [&](int i) { return per == 1 ? mine : tree_meta(p, i); };
+  int total;
+  const int excl = block_excl_scan<NW>(work, lds, total);
+  int *loc = lds + 2 * NW;  // located share: i, sub, off, q0, q1, ctx, start, end
+  int share = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+  share = max(kMinShare, round_up_block(share));
+  int cap = 0;
+  if (share == kMinShare) {
+    // pieces under each cap and, last, segments: at most eight blocks for every
+    // workgroup of the grid, so they fit 16 bits
+    constexpr int kPacked = kNumPieceCaps / 2 + 1;
+    uint32_t cnt[kPacked] = {};
+    int longest = 0;
+    for (int i = lo; i < hi; ++i) {
+      const TreeMeta r = meta(i);
+      const int m = r.groups * p.hkv;
+#pragma unroll
+      for (int c = 0; c < kNumPieceCaps; ++c)
+        cnt[c / 2] += (uint32_t)(m * seg_pieces(r.seg, piece_cap(c))) << (16 * (c % 2));
+      cnt[kPacked - 1] += (uint32_t)m << 16;
+      longest = max(longest, r.seg);
+    }
+    uint32_t *red = reinterpret_cast<uint32_t *>(loc + 8);  // [kPacked + 1][NW]
+    const int lane = tid % kWave, wave = tid / kWave;
+#pragma unroll
+    for (int c = 0; c <= kPacked; ++c) {
+      const int v = c < kPacked ? wave_incl_scan((int)cnt[c < kPacked ? c : 0]) : wave_max(longest);
+      if (lane == kWave - 1) red[c * NW + wave] = (uint32_t)v;
+    }
+    __syncthreads();
+    const int one_per_cu = min(p.num_cu, (int)gridDim.x);
+    longest = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) longest = max(longest, (int)red[kPacked * NW + w]);
+    int pieces[kNumPieceCaps + 1];
+#pragma unroll
+    for (int c = 0; c <= kNumPieceCaps; ++c) {
+      int t = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) t += (int)(red[c / 2 * NW + w] >> (16 * (c % 2)) & 0xFFFFu);
+      pieces[c] = t;
+    }
+#pragma unroll
+    for (int c = kNumPieceCaps - 1; c >= 0; --c)
+      if (pieces[c] <= one_per_cu || (c == 0 && cap == 0 && pieces[c] <= (int)gridDim.x))
+        cap = piece_cap(c);
+    const int all = pieces[kNumPieceCaps];  // segments
+    const CutRule rule = NW == 8 && D == 128
+                             ? CutRule{3, 5, 5}
+                             : cut_rule((float)live * (float)(p.group * p.hkv * D), (float)all);
+    const int spare = min(p.num_cu * rule.cu_sixteenths / 16, (int)gridDim.x) - all;
+    if (spare > 0 && longest > rule.whole_blocks * kBlockKeys) {
+      const int blocks = max(rule.min_blocks, max((longest / kBlockKeys + kMaxMerge - 1) / kMaxMerge,
+                                                  (total / kBlockKeys + spare - 1) / spare));
+      if (blocks < 8) cap = blocks * kBlockKeys;
+    }
+  }
+  const bool seg_mode = cap > 0;
+  const int lead = seg_mode ? 0 : kLeadKeys;
+  int my_pc = 0, total_pc = 0, excl_pc = 0;          // pieces (small batches)
+  int my_v = work, total_v = total, excl_v = excl;  // keys with lead-ins (stream-K)
+  if (seg_mode) {
+    for (int i = lo; i < hi; ++i) {
+      const TreeMeta r = meta(i);
+      my_pc += r.groups * p.hkv * seg_pieces(r.seg, cap);
+    }
+    excl_pc = block_excl_scan<NW>(my_pc, lds + NW, total_pc);
+  } else {
+    my_v = work + lead * segs;
+    excl_v = block_excl_scan<NW>(my_v, lds + NW, total_v);
+    share = (total_v + (int)gridDim.x - 1) / (int)gridDim.x;
+    share = max(kMinShare, round_up_block(share));
+  }
+  if (blockIdx.x == 0) {
+    int acc = excl_v, acc_pc = excl_pc;
+    for (int i = lo; i < hi; ++i) {
+      const TreeMeta r = meta(i);
+      const int m = r.groups * p.hkv;
+      p.plan[i] = acc;
+      p.plan[B + 2 + i] = acc_pc;
+      acc += m * (r.seg + lead);
+      if (seg_mode) acc_pc += m * seg_pieces(r.seg, cap);
+    }
+    if (tid == 0) {
+      p.plan[B] = total_v;
+      p.plan[B + 1] = seg_mode ? -cap : share;  // negative: the small-batch cap
+      p.plan[2 * B + 2] = total_pc;
+    }
+  }
+  const int b = (int)blockIdx.x;
+  int start = total_v, end = total_v;
+  if (!seg_mode) {
+    const int skew = share_skew(share);
+    start = min(total_v, share_begin(b, share, skew));
+    end = min(total_v, share_begin(b + 1, share, skew));
+  }
+  // the thread whose requests contain this workgroup's share locates it
+  const bool here = seg_mode ? excl_pc <= b && b < excl_pc + my_pc
+                             : start < total_v && excl_v <= start && start < excl_v + my_v;
+  if (here) {
+    int acc = excl_v, acc_pc = excl_pc;
+    for (int i = lo; i < hi; ++i) {
+      const TreeMeta r = meta(i);
+      const int m = r.groups * p.hkv, segv = r.seg + lead;
+      const int n = seg_mode ? seg_pieces(r.seg, cap) : 0;
+      int sub = -1, off = 0, s0 = 0, s1 = 0;
+      if (seg_mode) {
+        if (b < acc_pc + m * n) {
+          const int rel = b - acc_pc;
+          sub = rel / n;
+          const int q = rel % n;
+          off = piece_begin(r.seg, n, q);
+          s0 = acc + sub * r.seg + off;
+          s1 = s0 + piece_begin(r.seg, n, q + 1) - off;
+        }
+      } else if (start < acc + m * segv) {
+        const int rel = start - acc;
+        sub = rel / segv;
+        off = rel % segv;
+        s0 = start;
+        s1 = end;
+      }
+      if (sub >= 0) {
+        loc[0] = i;
+        loc[1] = sub;
+        loc[2] = off;
+        loc[3] = r.q0;
+        loc[4] = r.q0 + r.k;
+        loc[5] = r.ctx;
+        loc[6] = s0;
+        loc[7] = s1;
+        break;
+      }
+      acc += m * segv;
+      acc_pc += m * n;
+    }
+  }
+  __syncthreads();
+  auto uni = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const bool has = uni(seg_mode ? b < total_pc : start < total_v) != 0;
+  TreeShare sh;
+  sh.lead = uni(lead);
+  sh.start = has ? uni(loc[6]) : 0;
+  sh.end = has ? uni(loc[7]) : 0;
+  sh.i = uni(loc[0]);
+  sh.sub = uni(loc[1]);
+  sh.off = uni(loc[2]);
+  const int q0 = uni(loc[3]), q1 = uni(loc[4]), ctx = uni(loc[5]);
+  sh.first = tree_meta(p, q0, q1, ctx);
+  return sh;
+}
+
+// ------------------------------------------------------------------------ pieces
+// A piece: the workgroup's keys [key_begin, key_end) of request i, KV head g, row
+// group rg.
+struct TreePiece {
+  int i, g, rg, key_begin, key_end, slot, prio_end;
+  bool complete;
+  TreeMeta rq;
+  int rows;  // of the row group
+};
+
+// The wave's query operands and its rows' masks.
+template <int D, int TW>
+struct TreeQ {
+  bf16x8 r[TW][D / 32];
+  unsigned long long mask[TW];
+};
+
+// A row past the live ones loads row 0 of the request and is zeroed.
+template <int D, int TW>
+__device__ __forceinline__ void load_tree_q(const TreeParams &p, const TreePiece &x, int tile0,
+                                            int lane, TreeQ<D, TW> &qv) {
+  const int kq = lane >> 4, n = lane & 15;
+  const int lg = __builtin_ctz(p.group);
+  u32x4 w[TW][D / 32];
+  bool valid[TW];
+#pragma unroll
+  for (int t = 0; t < TW; ++t) {
+    const int rr = (tile0 + t) * 16 + n;
+    valid[t] = rr < x.rows;
+    const int at = valid[t] ? x.rg * p.group_rows + rr : 0;
+    const int j = at >> lg, hh = at & (p.group - 1);
+    qv.mask[t] = p.masks ? p.masks[x.rq.q0 + j] : (2ull << j) - 1;
+    const uint16_t *row = p.q + ((size_t)(x.rq.q0 + j) * p.hq + (size_t)x.g * p.group + hh) * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+      w[t][c] = *reinterpret_cast<const u32x4 *>(row + 32 * c + 8 * kq);
+  }
+#pragma unroll
+  for (int t = 0; t < TW; ++t) {
+    const uint32_t keep = valid[t] ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+      qv.r[t][c] = as_bf16x8(__builtin_bit_cast(uint4, w[t][c] & u32x4{keep, keep, keep, keep}));
+  }
+}
+
+// Masks of a step that holds keys past the context.  Element (h, q) of a lane is key
+// t0 + 16h + 4*(lane>>4) + q.  V cells of keys at or past se are zeroed.
+template <int TW, int NE>
+__device__ __forceinline__ void tree_mask(int t0, int se, int ctx,
+                                          const unsigned long long (&mask)[TW], int lane,
+                                          Scores<TW> &s, VRegs<NE> &v) {
+  const int kq = lane >> 4;
+  const int node = t0 - ctx;  // of key t0: negative in the context
+  const uint32_t inside = se - t0 >= 32 ? 0xFFFFFFFFu : (1u << (se - t0)) - 1;
+#pragma unroll
+  for (int t = 0; t < TW; ++t) {
+    uint32_t seen;  // bit b: the row sees key t0 + b
+    if (node >= 0)
+      seen = (uint32_t)(mask[t] >> node);
+    else if (node > -32)
+      seen = (uint32_t)mask[t] << -node | ((1u << -node) - 1);
+    else
+      seen = 0xFFFFFFFFu;
+    seen = (seen & inside) >> (4 * kq);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (!(seen >> (16 * h + q) & 1)) s.x[t][h][q] = -INFINITY;
+  }
+  const int tb = t0 + 16 * (kq & 1) + 8 * (kq >> 1);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t keep = (tb + 2 * w < se ? 0x0000FFFFu : 0u) |
+                          (tb + 2 * w + 1 < se ? 0xFFFF0000u : 0u);
+#pragma unroll
+    for (int u = 0; u < NE; ++u) v.x[u][w] &= keep;
+  }
+}
+
+// Whether any of the wave's V cells is an infinity or NaN.
+template <int NE>
+__device__ __forceinline__ bool any_not_finite(const VRegs<NE> &v) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int u = 0; u < NE; ++u)
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v.x[u][w] & 0x7FFF7FFFu));
+  return __builtin_amdgcn_ballot_w64(top[0] >= 0x7F80 || top[1] >= 0x7F80) != 0;
+}
+
+// Takes those cells out of v.
+template <int NE>
+__device__ __forceinline__ void take_out(VRegs<NE> &v) {
+#pragma unroll
+  for (int u = 0; u < NE; ++u)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t x = v.x[u][w];
+      v.x[u][w] = x & (((x & 0x7F80u) == 0x7F80u ? 0u : 0x0000FFFFu) |
+                       ((x & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u));
+    }
+}
+// Adds them, read from the ring once more, to a tile's outputs: to the rows whose
+// weight of the key is not 0.
+template <int NE>
+__device__ __forceinline__ void bring_back(const char *vb, bf16x8 ph, f32x4 (&o)[NE]) {
+  const uint4 weights = __builtin_bit_cast(uint4, ph);
+  const uint32_t pw[4] = {weights.x, weights.y, weights.z, weights.w};
+  uint32_t sees[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    sees[w] = (pw[w] & 0x7FFFu ? 0x3F80u : 0u) | (pw[w] & 0x7FFF0000u ? 0x3F800000u : 0u);
+  const bf16x8 sb = as_bf16x8(make_uint4(sees[0], sees[1], sees[2], sees[3]));
+#pragma unroll
+  for (int u = 0; u < NE; ++u) {
+    asm volatile("" ::: "memory");  // one block at a time: this path is to cost no registers
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(vb + 512 * u);
+#pragma unroll
+    for (int c = 1; c <= 3; ++c) {
+      // +inf, -inf, NaN
+      auto is = [&](uint32_t b) { return c == 3 ? (b & 0x7FFFu) > 0x7F80u : b == (c == 1 ? 0x7F80u : 0xFF80u); };
+      uint32_t one[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        one[w] = (is(x[w] & 0xFFFFu) ? 0x3F80u : 0u) | (is(x[w] >> 16) ? 0x3F800000u : 0u);
+      const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          as_bf16x8(make_uint4(one[0], one[1], one[2], one[3])), sb, f32x4{0.f, 0.f, 0.f, 0.f}, 0,
+          0, 0);
+      const float add = c == 1 ? INFINITY : (c == 2 ? -INFINITY : NAN);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (n[q] > 0.f) o[u][q] += add;
+    }
+  }
+}
+
+// -------------------------------------------------------------------------- ring
+struct TreeRing {
+  const int *ids;       // LDS: page ids of the sub-piece
+  const char *kbase;    // K tile of page 0, this KV head, plus the lane's offset
+  const char *vbase;    // V likewise
+  const uint8_t *scales;  // K scales of page 0, this KV head (8-bit cache)
+  uint32_t page_bytes, scale_bytes;
+  int ns;               // stages
+  int sb, se, ctx;      // first key, end of the keys, committed context
+  int prio_end;         // key at which the wave priority returns to the default
+};
+
+// A wave's tiles of one stage on their way to LDS: bf16 cells, or codes with the
+// page's sixteen scales.
+template <int D, int NW, bool kFp8>
+struct TreeStage {
+  u32x4 x[Ring<D, NW>::kTiles][kFp8 ? D / 64 : D / 32];
+  u32x4 e[Ring<D, NW>::kTiles];
+};
+
+// As ring_load in attn.hip: past the last stage page 0 is read and not used.
+template <int D, int NW, bool kFp8>
+__device__ __forceinline__ void tree_ring_load(const TreeRing &c, int b, int wave,
+                                               TreeStage<D, NW, kFp8> &r) {
+  using R = Ring<D, NW>;
+#pragma unroll
+  for (int q = 0; q < R::kTiles; ++q) {
+    const int at = R::kPages * min(b, c.ns - 1) + R::page(wave, q);
+    const int id = b < c.ns ? __builtin_amdgcn_readfirstlane(c.ids[at]) : 0;
+    const int kind = R::kind(wave, q);
+    const char *t = (kind ? c.vbase : c.kbase) + (size_t)(uint32_t)id * c.page_bytes;
+#pragma unroll
+    for (int x = 0; x < (kFp8 ? D / 64 : D / 32); ++x)
+      r.x[q][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(t + 1024 * x));
+    if (kFp8)
+      r.e[q] = *reinterpret_cast<const u32x4 *>(c.scales + (size_t)(uint32_t)id * c.scale_bytes +
+                                                kPage * kind);
+  }
+}
+
+// Two codes (the low or high half of a word) times a power of two, as bf16: exact.
+template <bool kHigh>
+__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, kHigh));
+}
+
+// Writes a wave's tile to the ring.  8-bit K: lane l holds sixteen dims of slot l & 15,
+// two of the ring's 8-dim chunks, under one scale.  8-bit V: a dim's sixteen slots, each
+// under its own.
+template <int D, int NW, bool kFp8>
+__device__ __forceinline__ void tree_ring_store(char *stage, int wave, int lane,
+                                                const TreeStage<D, NW, kFp8> &r) {
+  using R = Ring<D, NW>;
+#pragma unroll
+  for (int q = 0; q < R::kTiles; ++q) {
+    const int kind = R::kind(wave, q);
+    char *tile = stage + (kind * R::kPages + R::page(wave, q)) * R::kTile;
+    if constexpr (!kFp8) {
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+        *reinterpret_cast<u32x4 *>(tile + 1024 * x + 16 * lane) = r.x[q][x];
+    } else if (kind == 0) {
+      const int s = lane & 15;
+      const uint32_t lo = s & 4 ? r.e[q][1] : r.e[q][0], hi = s & 4 ? r.e[q][3] : r.e[q][2];
+      const uint32_t e = ((s & 8 ? hi : lo) >> (8 * (s & 3))) & 0xFFu;
+      const float scale = __uint_as_float(e << 23);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        char *to = tile + 16 * (2 * (4 * x + (lane >> 4)) * 16 + s);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t a = r.x[q][x][2 * h], b = r.x[q][x][2 * h + 1];
+          *reinterpret_cast<u32x4 *>(to + 256 * h) =
+              u32x4{bf16_of_codes<false>(a, scale), bf16_of_codes<true>(a, scale),
+                    bf16_of_codes<false>(b, scale), bf16_of_codes<true>(b, scale)};
+        }
+      }
+    } else {
+      float scale[16];
+#pragma unroll
+      for (int s = 0; s < 16; ++s)
+        scale[s] = __uint_as_float((r.e[q][s / 4] >> (8 * (s % 4)) & 0xFFu) << 23);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        const int dim = 64 * x + lane;
+        char *to = tile + 1024 * (dim / 32);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int code = (int)r.x[q][x][2 * h + y / 2];
+            const float *sc = scale + 8 * h + 2 * y;
+            const float a = y % 2 ? __builtin_amdgcn_cvt_f32_fp8(code, 2) : __builtin_amdgcn_cvt_f32_fp8(code, 0);
+            const float b = y % 2 ? __builtin_amdgcn_cvt_f32_fp8(code, 3) : __builtin_amdgcn_cvt_f32_fp8(code, 1);
+            w[y] = pack_bf16x2(a * sc[0], b * sc[1]);
+          }
+          *reinterpret_cast<u32x4 *>(to + 16 * v_unit(2 * (dim % 32) + h)) =
+              u32x4{w[0], w[1], w[2], w[3]};
+        }
+      }
+    }
+  }
+}
+
+// One stage in ring slot S: write it, load the stage kStages ahead, and after the
+// barrier compute the wave's steps of it.
+template <int D, int TW, int NE, int NW, bool kFp8, int S>
+__device__ __forceinline__ void tree_ring_step(const TreeRing &c, char *ring, int b, int wave,
+                                               int lane, TreeStage<D, NW, kFp8> &r,
+                                               const TreeQ<D, TW> &qv, const Role &role,
+                                               float scale_log2, RowState<TW, NE> &st) {
+  using R = Ring<D, NW>;
+  char *stage = ring + S * R::kStage;
+  tree_ring_store<D, NW, kFp8>(stage, wave, lane, r);
+  tree_ring_load<D, NW, kFp8>(c, b + R::kStages, wave, r);
+  __syncthreads();
+  if (c.sb + b * R::kKeys >= c.prio_end) __builtin_amdgcn_s_setprio(0);
+  if (!role.active) return;
+  const int kq = lane >> 4, m = lane & 15;
+  const char *vb = stage + (R::kPages + (kq & 1)) * R::kTile + 16 * v_unit(2 * m + (kq >> 1)) +
+                   512 * role.e_lo;
+#pragma unroll 1
+  for (int sub = 0; sub < R::kSteps; ++sub) {
+    const int t0 = c.sb + b * R::kKeys + sub * kBlockKeys;
+    if (t0 >= c.se) break;
+    KRegs<D> k;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+        k.x[h][x] = *reinterpret_cast<const u32x4 *>(
+            stage + (sub * 2 + h) * R::kTile + 1024 * x + 16 * lane);
+    Scores<TW> s;
+    step_scores<D, TW>(k, qv, s);
+    VRegs<NE> v;
+#pragma unroll
+    for (int u = 0; u < NE; ++u)
+      v.x[u] = *reinterpret_cast<const u32x4 *>(vb + sub * 2 * R::kTile + 512 * u);
+    bool odd = false;
+    if (t0 + kBlockKeys > min(c.ctx, c.se)) {
+      tree_mask<TW, NE>(t0, c.se, c.ctx, qv.mask, lane, s, v);
+      odd = any_not_finite(v);
+      if (odd) take_out(v);
+    }
+    step_update<TW, NE>(s, v, scale_log2, st, [&](int t, bf16x8 ph) {
+      if (odd) bring_back(vb + sub * 2 * R::kTile, ph, st.o[t]);
+    });
+  }
+}
+
+template <int D, int TW, int NE, int NW, bool kFp8>
+__device__ __forceinline__ void tree_ring_run(const TreeRing &c, char *ring, int wave, int lane,
+                                              const TreeQ<D, TW> &qv, const Role &role,
+                                              float scale_log2, RowState<TW, NE> &st) {
+  constexpr int kStages = Ring<D, NW>::kStages;
+  TreeStage<D, NW, kFp8> r[kStages];
+  // in stage order (the empty asm keeps the compiler from reordering them), so that
+  // each step waits only for its own stage
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) {
+    tree_ring_load<D, NW, kFp8>(c, s, wave, r[s]);
+    asm volatile("" ::: "memory");
+  }
+  for (int b = 0; b < c.ns; b += kStages) {
+    tree_ring_step<D, TW, NE, NW, kFp8, 0>(c, ring, b, wave, lane, r[0], qv, role, scale_log2, st);
+    tree_ring_step<D, TW, NE, NW, kFp8, 1>(c, ring, b + 1, wave, lane, r[1], qv, role, scale_log2, st);
+    tree_ring_step<D, TW, NE, NW, kFp8, 2>(c, ring, b + 2, wave, lane, r[2], qv, role, scale_log2, st);
+  }
+}
+
+// Writes NE d blocks from e_lo of a finished row tile: bf16 output when the piece is
+// the whole segment, else the fp32 partial in this workgroup's slot (0: the segment
+// where its share starts, 1: where it ends).
+template <int D, int NE>
+__device__ __forceinline__ void write_tree_rows(const TreeParams &p, const TreePiece &x, int rt,
+                                                int e_lo, int lane, float m, float l,
+                                                const f32x4 (&o)[NE]) {
+  const int kq = lane >> 4;
+  const int rr = rt * 16 + (lane & 15);
+  if (rr >= x.rows) return;
+  const int dim = 16 * e_lo + 4 * kq;
+  if (x.complete) {
+    const int at = x.rg * p.group_rows + rr;
+    const int j = at >> __builtin_ctz(p.group), hh = at & (p.group - 1);
+    const size_t row = (size_t)(x.rq.q0 + j) * p.hq + (size_t)x.g * p.group + hh;
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees no key is 0
+#pragma unroll
+    for (int u = 0; u < NE; ++u) {
+      uint2 w;
+      w.x = pack_bf16x2(o[u][0] * inv, o[u][1] * inv);
+      w.y = pack_bf16x2(o[u][2] * inv, o[u][3] * inv);
+      *reinterpret_cast<uint2 *>(p.out + row * D + dim + 16 * u) = w;
+    }
+  } else {
+    const size_t prow = ((size_t)blockIdx.x * 2 + x.slot) * p.group_rows + rr;
+#pragma unroll
+    for (int u = 0; u < NE; ++u)
+      *reinterpret_cast<f32x4 *>(p.part_o + prow * D + dim + 16 * u) = o[u];
+    if (e_lo == 0 && kq == 0) p.part_ml[prow] = make_float2(m, l);
+  }
+}
+
+// Wave roles as run_piece in attn.hip: with NE < D/16 d blocks the waves split one
+// tile's dims (or two tiles', half of the waves each), else each has TW tiles to itself.
+template <int D, int TW, int NE, int NW, bool kFp8>
+__device__ __forceinline__ void run_tree_piece(const TreeParams &p, char *buf, int *ids,
+                                               const TreePiece &x, int wave, int lane) {
+  using R = Ring<D, NW>;
+  constexpr int kParts = D / 16 / NE;  // waves to a tile
+  constexpr int kCell = kFp8 ? 1 : 2;
+  Role role;
+  role.tile0 = wave / kParts * TW;
+  role.e_lo = wave % kParts * NE;
+  role.active = role.tile0 * 16 < x.rows;
+  RowState<TW, NE> st;
+  TreeQ<D, TW> qv;
+  load_tree_q<D, TW>(p, x, role.tile0, lane, qv);
+  clear_state<TW, NE>(st);
+  TreeRing c;
+  c.ids = ids;
+  c.page_bytes = (uint32_t)(2 * p.hkv * kPage * D * kCell);
+  c.kbase = reinterpret_cast<const char *>(p.kv) + (size_t)x.g * kPage * D * kCell + 16 * lane;
+  c.vbase = reinterpret_cast<const char *>(p.kv) + (size_t)(p.hkv + x.g) * kPage * D * kCell +
+            16 * (kFp8 ? lane : v_unit_inv(lane));
+  c.scales = p.scales + (size_t)x.g * 2 * kPage;
+  c.scale_bytes = (uint32_t)(p.hkv * 2 * kPage);
+  c.ctx = x.rq.ctx;
+  c.prio_end = x.prio_end;
+  for (int sb = x.key_begin; sb < x.key_end; sb += kSubKeys) {
+    const int se = min(x.key_end, sb + kSubKeys);
+    c.sb = sb;
+    c.se = se;
+    c.ns = (se - sb + R::kKeys - 1) / R::kKeys;
+    // an id outside [0, num_pages) breaks the contract and reads page 0 instead; pages
+    // past the sub-piece read page 0 and are masked
+    const int npg = (se - sb + kPage - 1) / kPage;
+    const int32_t *pt = p.page_table + (size_t)x.i * p.max_pages + sb / kPage;
+    if (sb > x.key_begin) __syncthreads();  // the last ids and stages have been read
+    for (int t = threadIdx.x; t < R::kPages * c.ns; t += NW * kWave) {
+      const int id = t < npg ? pt[t] : 0;
+      ids[t] = (unsigned)id < (unsigned)p.num_pages ? id : 0;
+    }
+    __syncthreads();
+    tree_ring_run<D, TW, NE, NW, kFp8>(c, buf, wave, lane, qv, role, p.scale_log2, st);
+  }
+  if (!role.active) return;
+#pragma unroll
+  for (int t = 0; t < TW; ++t)
+    write_tree_rows<D, NE>(p, x, role.tile0 + t, role.e_lo, lane, st.m[t], row_sum4(st.l[t]),
+                           st.o[t]);
+}
+
+// NW waves, each with up to kTW row tiles: group_rows = 16 * NW * kTW.
+constexpr int tree_waves_per_simd(int D, int NW, int kTW) {
+  return D == 64 && NW == 4 ? (kTW == 1 ? 4 : (kTW == 2 ? 3 : 2)) : 2;
+}
+template <int D, int NW, int kTW, bool kFp8>
+__global__ __launch_bounds__(NW *kWave, tree_waves_per_simd(D, NW, kTW)) void tree_attn_kernel(
+    TreeParams p) {
+  __shared__ __attribute__((aligned(1024))) char buf[Ring<D, NW>::kBytes];
+  __shared__ int ids[kSubPages];
+  __shared__ int lds_plan[2 * NW + 8 + (kNumPieceCaps / 2 + 2) * NW];
+
+  const TreeShare sh = tree_plan<D, NW>(p, lds_plan);
+  if (sh.start >= sh.end) return;
+  int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  int lane = threadIdx.x % kWave;
+
+  // the workgroups placed after the first on a CU, over half of their share
+  const bool boost = (int)blockIdx.x >= p.num_cu;
+  if (boost) __builtin_amdgcn_s_setprio(1);
+  const int boost_end = boost ? sh.start + (int)((long long)(sh.end - sh.start) * kBoostPct / 100) : -1;
+
+  TreePiece x;
+  x.i = sh.i;
+  x.rq = sh.first;
+  int sub = sh.sub, off = sh.off, pos = sh.start, piece = 0, i_meta = sh.i;
+  while (pos < sh.end && x.i < p.num_reqs) {
+    if (x.i != i_meta) {
+      const int q0 = __builtin_amdgcn_readfirstlane(p.cu[x.i]);
+      const int q1 = __builtin_amdgcn_readfirstlane(p.cu[x.i + 1]);
+      const int ctx = __builtin_amdgcn_readfirstlane(p.ctx[x.i]);
+      x.rq = tree_meta(p, q0, q1, ctx);
+      i_meta = x.i;
+    }
+    if (x.rq.seg == 0) {  // no rows, or metadata out of range: no keys in the plan
+      ++x.i;
+      continue;
+    }
+    const int segv = x.rq.seg + sh.lead;
+    const int take = min(segv - off, sh.end - pos);
+    x.key_begin = max(off - sh.lead, 0);
+    x.key_end = min(x.rq.len, off + take - sh.lead);
+    if (x.key_end <= x.key_begin) break;  // the share ends inside the lead-in
+    x.complete = off <= sh.lead && off + take == segv;
+    x.slot = piece == 0 ? 0 : 1;
+    x.prio_end = boost ? x.key_begin + boost_end - pos : 0x7FFFFFFF;
+    x.g = sub / x.rq.groups;
+    x.rg = sub % x.rq.groups;
+    x.rows = min(p.group_rows, p.group * x.rq.k - x.rg * p.group_rows);
+    if (piece > 0) __syncthreads();  // the last piece's LDS has been read
+
+    asm volatile("" : "+v"(lane), "+s"(wave));  // no offsets of all the forms ahead of the loop
+    const int nt = (x.rows + 15) / 16;  // row tiles
+    constexpr int kBlocks = D / 16;
+    if (NW == 4 && nt == 1)
+      run_tree_piece<D, 1, kBlocks / 4, NW, kFp8>(p, buf, ids, x, wave, lane);
+    else if (NW == 4 && nt == 2)
+      run_tree_piece<D, 1, kBlocks / 2, NW, kFp8>(p, buf, ids, x, wave, lane);
+    else if (kTW == 1 || nt <= NW)
+      run_tree_piece<D, 1, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+    else if (kTW == 2 || nt <= 2 * NW)
+      run_tree_piece<D, 2, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+    else
+      run_tree_piece<D, kTW, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+
+    pos += take;
+    off += take;
+    ++piece;
+    if (off == segv) {
+      off = 0;
+      if (++sub == x.rq.groups * p.hkv) {
+        sub = 0;
+        ++x.i;
+      }
+    }
+  }
+}
+
+// Merges the partials of segments cut at share boundaries, in workgroup order, and
+// zeroes the tail rows.  Workgroup (x, y, i) owns kCombThreads / (D/4) rows of segment y
+// of request i; a thread four dims of a row.
+template <int D>
+__global__ __launch_bounds__(kCombThreads) void tree_combine_kernel(TreeParams p) {
+  constexpr int kLanesPerRow = D / 4;
+  constexpr int kRows = kCombThreads / kLanesPerRow;
+  const int sub = blockIdx.y, i = blockIdx.z;
+  if (i == p.num_reqs) {
+    const int live = min(max(p.cu[p.num_reqs], 0), p.cap);
+    const long long total = (long long)(p.cap - live) * p.hq * (D / 8);
+    uint4 *tail = reinterpret_cast<uint4 *>(p.out + (size_t)live * p.hq * D);
+    const long long step = (long long)gridDim.x * gridDim.y * kCombThreads;
+    for (long long n = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * kCombThreads + threadIdx.x;
+         n < total; n += step)
+      tail[n] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  // one round trip: the empty asm uses every word before the first branch
+  int prefix = p.plan[i], share = p.plan[p.num_reqs + 1];
+  int pc_prefix = p.plan[p.num_reqs + 2 + i];
+  int cq0 = p.cu[i], cq1 = p.cu[i + 1], cctx = p.ctx[i];
+  asm volatile("" : "+s"(prefix), "+s"(share), "+s"(pc_prefix), "+s"(cq0), "+s"(cq1), "+s"(cctx));
+  const TreeMeta rq = tree_meta(p, cq0, cq1, cctx);
+  if (sub >= rq.groups * p.hkv) return;
+  const int seg = rq.seg + (share > 0 ? kLeadKeys : 0);
+  const int start = prefix + sub * seg;
+  const int skew = share > 0 ? share_skew(share) : 0;
+  int b0, b1;
+  if (share <= 0) {
+    const int n = seg_pieces(seg, -share);
+    b0 = pc_prefix + sub * n;
+    b1 = b0 + n - 1;
+  } else {
+    b0 = share_owner(start + kLeadKeys, share, skew);
+    b1 = share_owner(start + seg - 1, share, skew);
+  }
+  if (b0 == b1) return;  // one workgroup held the whole segment
+  const int g = sub / rq.groups, rg = sub % rq.groups;
+  const int rr = blockIdx.x * kRows + threadIdx.x / kLanesPerRow;
+  if (rr >= min(p.group_rows, p.group * rq.k - rg * p.group_rows)) return;
+  const int d4 = threadIdx.x % kLanesPerRow;
+  const int at = rg * p.group_rows + rr;
+  const int j = at >> __builtin_ctz(p.group), hh = at & (p.group - 1);
+  const size_t row = (size_t)(rq.q0 + j) * p.hq + (size_t)g * p.group + hh;
+  const int n_parts = b1 - b0 + 1;
+  auto prow = [&](int u) -> size_t {
+    const int b = b0 + u;
+    const int slot = share <= 0 || share_begin(b, share, skew) >= start ? 0 : 1;
+    return ((size_t)b * 2 + slot) * p.group_rows + rr;
+  };
+  float mx = -INFINITY;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float den = 0.f;
+  if (n_parts > 8)
+    for (int u0 = 0; u0 < n_parts; u0 += 8) {
+      float m8[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        m8[u] = u0 + u < n_parts ? p.part_ml[prow(u0 + u)].x : -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) mx = fmaxf(mx, m8[u]);
+    }
+  for (int u0 = 0; u0 < n_parts; u0 += 8) {
+    float2 l8[8];
+    f32x4 o8[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool in = u0 + u < n_parts;
+      const size_t pr = prow(u0 + u);
+      l8[u] = in ? p.part_ml[pr] : make_float2(-INFINITY, 0.f);
+      o8[u] = in ? *reinterpret_cast<const f32x4 *>(p.part_o + pr * D + 4 * d4)
+                 : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (n_parts <= 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) mx = fmaxf(mx, l8[u].x);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = exp2f(l8[u].x - mx);
+      den += w * l8[u].y;
+      acc += w * o8[u];
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  uint2 w2;
+  w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<uint2 *>(p.out + row * D + 4 * d4) = w2;
+}
+
+// ------------------------------------------------------------------------- masks
+// One wave per request, lane j node j: what a node sees is itself and what its parent
+// sees, closed by doubling (six rounds for 64 nodes).  A parent that does not come before
+// its node makes the node a root.
+__global__ __launch_bounds__(kWave) void tree_masks_kernel(const int32_t *parents,
+                                                          const int32_t *cu, const int32_t *ctx,
+                                                          unsigned long long *masks,
+                                                          int32_t *positions, int32_t cap) {
+  const int i = blockIdx.x, j = threadIdx.x;
+  const int o = cu[i], k = cu[i + 1] - o;
+  if (k <= 0 || k > kMaxNodes || o < 0 || o + k > cap) return;
+  int up = j < k ? parents[o + j] : -1;
+  if (up < 0 || up >= j) up = -1;
+  unsigned long long mask = 1ull << j;
+  int depth = up >= 0 ? 1 : 0;
+#pragma unroll
+  for (int round = 0; round < 6; ++round) {
+    const int from = max(up, 0);
+    const unsigned long long m = __shfl(mask, from);
+    const int d = __shfl(depth, from), u = __shfl(up, from);
+    if (up >= 0) {
+      mask |= m;
+      depth += d;
+      up = u;
+    }
+  }
+  if (j < k) {
+    masks[o + j] = mask;
+    if (positions) positions[o + j] = ctx[i] + depth;
+  }
+}
+
+// The split kernel for a batch's dims: as many row tiles as the largest tree has, up to
+// what a workgroup's registers hold.
+struct TreeKernel {
+  int index;  // of the form, below kTreeKernels
+  void (*fn)(TreeParams);
+  int threads, group_rows, max_grid;
+};
+constexpr int kTreeKernels = 12;
+template <bool kFp8>
+TreeKernel tree_kernel(const dsv_tree_dims &d) {
+  const int tiles = (d.num_q_heads / d.num_kv_heads * d.max_nodes + 15) / 16;
+  constexpr int k4 = 4 * kWave, k8 = 8 * kWave, at = kFp8 ? kTreeKernels / 2 : 0;
+  if (d.head_dim == 128) {
+    if (tiles <= 4) return {at, tree_attn_kernel<128, 4, 1, kFp8>, k4, 64, 512};
+    if (tiles <= 8) return {at + 1, tree_attn_kernel<128, 4, 2, kFp8>, k4, 128, 512};
+    return {at + 2, tree_attn_kernel<128, 8, 2, kFp8>, k8, 256, 256};
+  }
+  if (tiles <= 4) return {at + 3, tree_attn_kernel<64, 4, 1, kFp8>, k4, 64, 1024};
+  if (tiles <= 8) return {at + 4, tree_attn_kernel<64, 4, 2, kFp8>, k4, 128, 768};
+  return {at + 5, tree_attn_kernel<64, 4, 4, kFp8>, k4, 256, 512};
+}
+TreeKernel tree_kernel_of(const dsv_tree_dims &d) {
+  return d.kv_dtype == DSV_FP8 ? tree_kernel<true>(d) : tree_kernel<false>(d);
+}
+
+int32_t tree_grid_cap(const dsv_tree_dims &d, const TreeKernel &k) {
+  const int rows = d.num_q_heads / d.num_kv_heads * d.max_nodes;
+  const long long groups = (rows + k.group_rows - 1) / k.group_rows;
+  const long long blocks = (long long)d.num_reqs * d.num_kv_heads * groups *
+                           ((d.max_kv_len + kBlockKeys - 1) / kBlockKeys);
+  return (int32_t)(blocks < k.max_grid ? blocks : k.max_grid);
+}
+
+}  // namespace
+
+// Workgroups the current device holds at once (cached per device and form), capped; 0
+// if a device query failed.
+int32_t tree_grid(const dsv_tree_dims &d) {
+  static std::atomic<int> cache[64][kTreeKernels];
+  const TreeKernel k = tree_kernel_of(d);
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 0;
+  int resident = cache[dev][k.index].load(std::memory_order_relaxed);
+  if (resident <= 0) {
+    int per_cu = 0;
+    const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(
+        &per_cu, reinterpret_cast<const void *>(k.fn), k.threads, 0);
+    resident = attn_num_cu() * per_cu;
+    if (e != hipSuccess || resident <= 0) {
+      (void)hipGetLastError();
+      return 0;
+    }
+    cache[dev][k.index].store(resident, std::memory_order_relaxed);
+  }
+  const int32_t cap = tree_grid_cap(d, k);
+  return resident < cap ? resident : cap;
+}
+
+TreeWorkspace tree_workspace_layout(const dsv_tree_dims &d) {
+  const TreeKernel k = tree_kernel_of(d);
+  TreeWorkspace w;
+  w.group_rows = k.group_rows;
+  const int rows = d.num_q_heads / d.num_kv_heads * d.max_nodes;
+  w.row_groups = (rows + k.group_rows - 1) / k.group_rows;
+  const size_t parts = (size_t)tree_grid_cap(d, k) * 2 * (size_t)k.group_rows;
+  w.plan_off = 0;
+  w.part_ml_off = align_up((size_t)(2 * d.num_reqs + 3) * sizeof(int32_t), 256);
+  w.part_o_off = align_up(w.part_ml_off + parts * sizeof(float2), 256);
+  w.total = align_up(w.part_o_off + parts * d.head_dim * sizeof(float), 256);
+  return w;
+}
+
+hipError_t launch_tree_attn(const TreeParams &p, const dsv_tree_dims &d, int32_t grid,
+                            hipStream_t s) {
+  const TreeKernel k = tree_kernel_of(d);
+  const int comb_rows = kCombThreads / (d.head_dim / 4);
+  const TreeWorkspace w = tree_workspace_layout(d);
+  const int rows = p.group * p.max_nodes < w.group_rows ? p.group * p.max_nodes : w.group_rows;
+  launch_kernel(k.fn, dim3(grid), dim3(k.threads), s, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  launch_kernel(d.head_dim == 128 ? tree_combine_kernel<128> : tree_combine_kernel<64>,
+                dim3((rows + comb_rows - 1) / comb_rows, p.hkv * w.row_groups, p.num_reqs + 1),
+                dim3(kCombThreads), s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_masks(const int32_t *parents, const int32_t *cu, const int32_t *ctx,
+                             unsigned long long *masks, int32_t *positions, int32_t num_reqs,
+                             int32_t cap, hipStream_t s) {
+  launch_kernel(tree_masks_kernel, dim3(num_reqs), dim3(kWave), s, parents, cu, ctx, masks,
+                positions, cap);
+  return hipGetLastError();
+}
+
+}  // namespace dsv
