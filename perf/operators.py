@@ -562,8 +562,10 @@ def _own_run(s):
         return s["k_out"], s["v_out"]
     if kind == "attn":
         if "ws" not in s:  # kept by the program from step to step
+            # no request is longer than its row of the page table
+            most = min(s["max_len"], PAGE * s["table"].shape[1])
             s["dims"] = dsv.tree_attn_dims(s["q"], s["pages"], s["table"], s["scales"],
-                                           max_nodes=s["max_nodes"], max_kv_len=s["max_len"])
+                                           max_nodes=s["max_nodes"], max_kv_len=most)
             s["ws"] = dsv.alloc_workspace(dsv.tree_attn_workspace_bytes(s["dims"]))
         dsv.tree_attn(s["q"], s["cu"], s["masks"], s["pages"], s["table"], s["ctx"], s["out"],
                       s["scales"], dims=s["dims"], workspace=s["ws"])
