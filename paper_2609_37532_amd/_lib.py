@@ -137,6 +137,10 @@ def _ptr(t) -> Optional[int]:
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         import torch
+        # the handle alone takes 0.1 us, a Stream object 2.7 us of a 9 us call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return int(raw(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     if isinstance(stream, int):
         return stream
