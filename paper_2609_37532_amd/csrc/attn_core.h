@@ -255,15 +255,16 @@ __device__ __forceinline__ void step_scores(const KRegs<D> &k, const QOps &qv, S
   }
 }
 
-// Online softmax and the PV product of one step.  `after(t, ph)` follows tile t's
-// products, with its weights as the PV operand.
-struct Nothing {
-  __device__ __forceinline__ void operator()(int, bf16x8) const {}
+// Online softmax and the PV product of one step.  A V whose rows have scales
+// (`VScale::kOn`: x[h][q] of the lane's keys) takes them in the weights.
+struct NoScale {
+  static constexpr bool kOn = false;
+  f32x4 x[2];
 };
-template <int TW, int NE, typename After = Nothing>
+template <int TW, int NE, typename VScale = NoScale>
 __device__ __forceinline__ void step_update(const Scores<TW> &s, const VRegs<NE> &v,
                                             float scale_log2, RowState<TW, NE> &st,
-                                            const After &after = After()) {
+                                            const VScale &scale = VScale()) {
   // a lane's own keys decide whether any row's maximum moves; only then are
   // the row's four lanes brought together
   bool jump = false;
@@ -310,6 +311,9 @@ __device__ __forceinline__ void step_update(const Scores<TW> &s, const VRegs<NE>
         pw[q] = __builtin_amdgcn_exp2f(
             __builtin_fmaf(s.x[t][h][q], scale_log2, -st.m[t]));
       psum[h] = (pw[0] + pw[1]) + (pw[2] + pw[3]);
+      if constexpr (VScale::kOn)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) pw[q] *= scale.x[h][q];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const uint32_t x = pack_bf16x2(pw[2 * w], pw[2 * w + 1]);
@@ -336,7 +340,6 @@ __device__ __forceinline__ void step_update(const Scores<TW> &s, const VRegs<NE>
     for (int u = 0; u < NE; ++u)
       st.o[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
           as_bf16x8(__builtin_bit_cast(uint4, v.x[u])), pl, st.o[t][u], 0, 0, 0);
-    after(t, ph);
   }
 }
 

@@ -16,14 +16,16 @@
 //    takes its row's 64-bit mask, shifted so that bit b is key t0 + b; other blocks are
 //    as in verify attention.
 //  * Nodes that a row does not see may hold anything, also infinities and NaN: a
-//    weight of 0 times such a V would be NaN in the matrix product.  Where a block of
-//    nodes holds one (a test of the block's V operands), its V cells that are not finite
-//    are taken out of the product and brought to the rows that see them by three
-//    products of ones and zeros.
+//    weight of 0 times such a V would be NaN in the matrix product.  V cells of node blocks
+//    that are not finite are therefore left out on the way to the ring, as are cells past
+//    the nodes, and noted; a piece that met one adds them, at its end and cell by cell, to
+//    the rows that see them.
 //  * An 8-bit cache is half the bytes.  Codes become bf16 on the way from the load
-//    registers to the LDS ring, their scale (a power of two) multiplied in, which is
-//    exact, so the ring and all after it are the bf16 cache's, and each code is converted
-//    once for all waves.
+//    registers to the LDS ring, which is exact, so the ring's layout and all after it are
+//    the bf16 cache's, and each code is converted once for all waves.  A K tile's lane
+//    holds dims of one slot, so K's scale goes into the conversion instruction; V's lane
+//    holds the slots of one dim, so V's scales, through LDS, go into the fp32 weights.
+//    Both are powers of two: exact.
 #include "attn_core.h"
 
 #include <atomic>
@@ -283,11 +285,11 @@ __device__ __forceinline__ void load_tree_q(const TreeParams &p, const TreePiece
 }
 
 // Masks of a step that holds keys past the context.  Element (h, q) of a lane is key
-// t0 + 16h + 4*(lane>>4) + q.  V cells of keys at or past se are zeroed.
-template <int TW, int NE>
+// t0 + 16h + 4*(lane>>4) + q.
+template <int TW>
 __device__ __forceinline__ void tree_mask(int t0, int se, int ctx,
                                           const unsigned long long (&mask)[TW], int lane,
-                                          Scores<TW> &s, VRegs<NE> &v) {
+                                          Scores<TW> &s) {
   const int kq = lane >> 4;
   const int node = t0 - ctx;  // of key t0: negative in the context
   const uint32_t inside = se - t0 >= 32 ? 0xFFFFFFFFu : (1u << (se - t0)) - 1;
@@ -307,113 +309,71 @@ __device__ __forceinline__ void tree_mask(int t0, int se, int ctx,
       for (int q = 0; q < 4; ++q)
         if (!(seen >> (16 * h + q) & 1)) s.x[t][h][q] = -INFINITY;
   }
-  const int tb = t0 + 16 * (kq & 1) + 8 * (kq >> 1);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t keep = (tb + 2 * w < se ? 0x0000FFFFu : 0u) |
-                          (tb + 2 * w + 1 < se ? 0xFFFF0000u : 0u);
-#pragma unroll
-    for (int u = 0; u < NE; ++u) v.x[u][w] &= keep;
-  }
-}
-
-// Whether any of the wave's V cells is an infinity or NaN.
-template <int NE>
-__device__ __forceinline__ bool any_not_finite(const VRegs<NE> &v) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  u16x2 top = {0, 0};
-#pragma unroll
-  for (int u = 0; u < NE; ++u)
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v.x[u][w] & 0x7FFF7FFFu));
-  return __builtin_amdgcn_ballot_w64(top[0] >= 0x7F80 || top[1] >= 0x7F80) != 0;
-}
-
-// Takes those cells out of v.
-template <int NE>
-__device__ __forceinline__ void take_out(VRegs<NE> &v) {
-#pragma unroll
-  for (int u = 0; u < NE; ++u)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t x = v.x[u][w];
-      v.x[u][w] = x & (((x & 0x7F80u) == 0x7F80u ? 0u : 0x0000FFFFu) |
-                       ((x & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u));
-    }
-}
-// Adds them, read from the ring once more, to a tile's outputs: to the rows whose
-// weight of the key is not 0.
-template <int NE>
-__device__ __forceinline__ void bring_back(const char *vb, bf16x8 ph, f32x4 (&o)[NE]) {
-  const uint4 weights = __builtin_bit_cast(uint4, ph);
-  const uint32_t pw[4] = {weights.x, weights.y, weights.z, weights.w};
-  uint32_t sees[4];
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-    sees[w] = (pw[w] & 0x7FFFu ? 0x3F80u : 0u) | (pw[w] & 0x7FFF0000u ? 0x3F800000u : 0u);
-  const bf16x8 sb = as_bf16x8(make_uint4(sees[0], sees[1], sees[2], sees[3]));
-#pragma unroll
-  for (int u = 0; u < NE; ++u) {
-    asm volatile("" ::: "memory");  // one block at a time: this path is to cost no registers
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(vb + 512 * u);
-#pragma unroll
-    for (int c = 1; c <= 3; ++c) {
-      // +inf, -inf, NaN
-      auto is = [&](uint32_t b) { return c == 3 ? (b & 0x7FFFu) > 0x7F80u : b == (c == 1 ? 0x7F80u : 0xFF80u); };
-      uint32_t one[4];
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        one[w] = (is(x[w] & 0xFFFFu) ? 0x3F80u : 0u) | (is(x[w] >> 16) ? 0x3F800000u : 0u);
-      const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          as_bf16x8(make_uint4(one[0], one[1], one[2], one[3])), sb, f32x4{0.f, 0.f, 0.f, 0.f}, 0,
-          0, 0);
-      const float add = c == 1 ? INFINITY : (c == 2 ? -INFINITY : NAN);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (n[q] > 0.f) o[u][q] += add;
-    }
-  }
 }
 
 // -------------------------------------------------------------------------- ring
+// What a wave needs to run the ring over one sub-piece.  Of every stage a wave loads one
+// tile: page wave >> 1, K or V by wave & 1.
+constexpr int kIdRegs = 4;  // windows of 64 stages whose page ids a wave holds
 struct TreeRing {
-  const int *ids;       // LDS: page ids of the sub-piece
-  const char *kbase;    // K tile of page 0, this KV head, plus the lane's offset
-  const char *vbase;    // V likewise
-  const uint8_t *scales;  // K scales of page 0, this KV head (8-bit cache)
+  const char *base;       // the wave's tile in page 0, plus the lane's offset
+  const uint8_t *scales;  // its scales in page 0, plus the lane's slot (8-bit cache)
   uint32_t page_bytes, scale_bytes;
-  int ns;               // stages
-  int sb, se, ctx;      // first key, end of the keys, committed context
-  int prio_end;         // key at which the wave priority returns to the default
+  u32x4 id;               // lane j of id[w]: the page of stage 64w + j
+  int ns;                 // stages
+  int sb, se, ctx;        // first key, end of the keys, committed context
+  int prio_end;           // key at which the wave priority returns to the default
+  int *not_finite;        // LDS: a V cell of a node was left out
 };
 
-// A wave's tiles of one stage on their way to LDS: bf16 cells, or codes with the
-// page's sixteen scales.
-template <int D, int NW, bool kFp8>
+// A wave's tile of one stage on its way to LDS: bf16 cells, or codes with the scale of
+// slot lane & 15.
+template <int D, bool kFp8>
 struct TreeStage {
-  u32x4 x[Ring<D, NW>::kTiles][kFp8 ? D / 64 : D / 32];
-  u32x4 e[Ring<D, NW>::kTiles];
+  u32x4 x[kFp8 ? D / 64 : D / 32];
+  uint32_t e;
 };
 
-// As ring_load in attn.hip: past the last stage page 0 is read and not used.
-template <int D, int NW, bool kFp8>
-__device__ __forceinline__ void tree_ring_load(const TreeRing &c, int b, int wave,
-                                               TreeStage<D, NW, kFp8> &r) {
-  using R = Ring<D, NW>;
+// A step's V scales by key, of the lane's eight keys.
+template <bool kFp8>
+struct VScales {
+  static constexpr bool kOn = kFp8;
+  f32x4 x[2];
+};
+
+// Page ids of the sub-piece's stages, each wave for its own tiles and straight into
+// registers: through LDS they took a barrier at the start and a wait in every step.  An
+// id outside [0, num_pages) breaks the contract and reads page 0 instead; pages past the
+// sub-piece read page 0 and are masked.
+template <int NW>
+__device__ __forceinline__ void load_ids(const TreeParams &p, int i, int wave, int lane,
+                                         TreeRing &c) {
+  constexpr int kPages = NW / 2;
+  const int32_t *pt = p.page_table + (size_t)i * p.max_pages + c.sb / kPage;
+  const int npg = (c.se - c.sb + kPage - 1) / kPage;
+  auto load = [&](int w) {
+    const int at = kPages * (64 * w + lane) + (wave >> 1);
+    const int id = at < npg ? pt[at] : 0;
+    return (unsigned)id < (unsigned)p.num_pages ? (uint32_t)id : 0u;
+  };
+  c.id = u32x4{load(0), load(1), load(2), load(3)};
+}
+
+// Loads the wave's tile of stage b.  Past the last stage it reads page 0 (in cache, never
+// used): the loop then has one shape, and the compiler can wait for exactly the stage
+// each step writes.
+template <int D, bool kFp8>
+__device__ __forceinline__ void tree_ring_load(const TreeRing &c, int b, TreeStage<D, kFp8> &r) {
+  const int w = b >> 6;
+  const u32x4 all = c.id;
+  const uint32_t lo = w & 1 ? all[1] : all[0], hi = w & 1 ? all[3] : all[2];
+  const int ids = (int)(w & 2 ? hi : lo);
+  const uint32_t id = b < c.ns ? __builtin_amdgcn_readlane(ids, b & 63) : 0;
+  const char *t = c.base + (size_t)id * c.page_bytes;
 #pragma unroll
-  for (int q = 0; q < R::kTiles; ++q) {
-    const int at = R::kPages * min(b, c.ns - 1) + R::page(wave, q);
-    const int id = b < c.ns ? __builtin_amdgcn_readfirstlane(c.ids[at]) : 0;
-    const int kind = R::kind(wave, q);
-    const char *t = (kind ? c.vbase : c.kbase) + (size_t)(uint32_t)id * c.page_bytes;
-#pragma unroll
-    for (int x = 0; x < (kFp8 ? D / 64 : D / 32); ++x)
-      r.x[q][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(t + 1024 * x));
-    if (kFp8)
-      r.e[q] = *reinterpret_cast<const u32x4 *>(c.scales + (size_t)(uint32_t)id * c.scale_bytes +
-                                                kPage * kind);
-  }
+  for (int x = 0; x < (kFp8 ? D / 64 : D / 32); ++x)
+    r.x[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(t + 1024 * x));
+  if (kFp8) r.e = c.scales[(size_t)id * c.scale_bytes];
 }
 
 // Two codes (the low or high half of a word) times a power of two, as bf16: exact.
@@ -422,76 +382,82 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, kHigh));
 }
 
+// Leaves out the cells of a V tile, the lane's sixteen or eight slots of a dim from key
+// on, that lie past the keys or are not finite, and notes the latter.
+template <bool kFp8>
+__device__ __forceinline__ u32x4 only_finite(u32x4 x, int key, int se, int *not_finite) {
+  bool found = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    constexpr int kPer = kFp8 ? 4 : 2;
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) {
+      const uint32_t cell = kFp8 ? 0xFFu << (8 * c) : 0xFFFFu << (16 * c);
+      const uint32_t special = kFp8 ? 0x7Fu << (8 * c) : 0x7F80u << (16 * c);
+      const bool in = key + kPer * w + c < se, odd = (x[w] & special) == special;
+      found |= in && odd;
+      x[w] &= in && !odd ? 0xFFFFFFFFu : ~cell;
+    }
+  }
+  if (found) *not_finite = 1;
+  return x;
+}
+
 // Writes a wave's tile to the ring.  8-bit K: lane l holds sixteen dims of slot l & 15,
-// two of the ring's 8-dim chunks, under one scale.  8-bit V: a dim's sixteen slots, each
-// under its own.
+// two of the ring's 8-dim chunks.  8-bit V: a dim's sixteen slots; the scales of the
+// stage's keys go to vscale.  A scale is its exponent's bits; 255, which no writer leaves
+// and a slot past the keys may hold, would be an infinity that turns weights of 0 to NaN.
 template <int D, int NW, bool kFp8>
-__device__ __forceinline__ void tree_ring_store(char *stage, int wave, int lane,
-                                                const TreeStage<D, NW, kFp8> &r) {
+__device__ __forceinline__ void tree_ring_store(const TreeRing &c, int b, char *stage,
+                                                float *vscale, int wave, int lane,
+                                                TreeStage<D, kFp8> &r) {
   using R = Ring<D, NW>;
+  static_assert(R::kTiles == 1, "one tile to a wave");
+  const int page = wave >> 1, kind = wave & 1;
+  char *tile = stage + (kind * R::kPages + page) * R::kTile;
+  const int t0 = c.sb + b * R::kKeys;
+  if (kind && t0 + R::kKeys > min(c.ctx, c.se)) {
+    const int key = t0 + kPage * page + (kFp8 ? 0 : 8 * (v_unit_inv(lane) & 1));
 #pragma unroll
-  for (int q = 0; q < R::kTiles; ++q) {
-    const int kind = R::kind(wave, q);
-    char *tile = stage + (kind * R::kPages + R::page(wave, q)) * R::kTile;
-    if constexpr (!kFp8) {
+    for (int x = 0; x < (kFp8 ? D / 64 : D / 32); ++x)
+      r.x[x] = only_finite<kFp8>(r.x[x], key, c.se, c.not_finite);
+  }
+  if constexpr (!kFp8) {
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x)
-        *reinterpret_cast<u32x4 *>(tile + 1024 * x + 16 * lane) = r.x[q][x];
-    } else if (kind == 0) {
-      const int s = lane & 15;
-      const uint32_t lo = s & 4 ? r.e[q][1] : r.e[q][0], hi = s & 4 ? r.e[q][3] : r.e[q][2];
-      const uint32_t e = ((s & 8 ? hi : lo) >> (8 * (s & 3))) & 0xFFu;
-      const float scale = __uint_as_float(e << 23);
+    for (int x = 0; x < D / 32; ++x) *reinterpret_cast<u32x4 *>(tile + 1024 * x + 16 * lane) = r.x[x];
+  } else {
+    const float scale = __uint_as_float(min(r.e, 254u) << 23);
+    const float by = kind ? 1.f : scale;
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) {
-        char *to = tile + 16 * (2 * (4 * x + (lane >> 4)) * 16 + s);
+    for (int x = 0; x < D / 64; ++x) {
+      const int dim = 64 * x + lane;  // V's; K: chunk 2 * (4x + lane / 16) of slot lane & 15
+      char *k_to = tile + 16 * (2 * (4 * x + (lane >> 4)) * 16 + (lane & 15));
+      char *v_to = tile + 1024 * (dim / 32);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t a = r.x[q][x][2 * h], b = r.x[q][x][2 * h + 1];
-          *reinterpret_cast<u32x4 *>(to + 256 * h) =
-              u32x4{bf16_of_codes<false>(a, scale), bf16_of_codes<true>(a, scale),
-                    bf16_of_codes<false>(b, scale), bf16_of_codes<true>(b, scale)};
-        }
-      }
-    } else {
-      float scale[16];
-#pragma unroll
-      for (int s = 0; s < 16; ++s)
-        scale[s] = __uint_as_float((r.e[q][s / 4] >> (8 * (s % 4)) & 0xFFu) << 23);
-#pragma unroll
-      for (int x = 0; x < D / 64; ++x) {
-        const int dim = 64 * x + lane;
-        char *to = tile + 1024 * (dim / 32);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[4];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int code = (int)r.x[q][x][2 * h + y / 2];
-            const float *sc = scale + 8 * h + 2 * y;
-            const float a = y % 2 ? __builtin_amdgcn_cvt_f32_fp8(code, 2) : __builtin_amdgcn_cvt_f32_fp8(code, 0);
-            const float b = y % 2 ? __builtin_amdgcn_cvt_f32_fp8(code, 3) : __builtin_amdgcn_cvt_f32_fp8(code, 1);
-            w[y] = pack_bf16x2(a * sc[0], b * sc[1]);
-          }
-          *reinterpret_cast<u32x4 *>(to + 16 * v_unit(2 * (dim % 32) + h)) =
-              u32x4{w[0], w[1], w[2], w[3]};
-        }
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t a = r.x[x][2 * h], b2 = r.x[x][2 * h + 1];
+        *reinterpret_cast<u32x4 *>(kind ? v_to + 16 * v_unit(2 * (dim % 32) + h) : k_to + 256 * h) =
+            u32x4{bf16_of_codes<false>(a, by), bf16_of_codes<true>(a, by),
+                  bf16_of_codes<false>(b2, by), bf16_of_codes<true>(b2, by)};
       }
     }
+    if (kind && lane < kPage) vscale[kPage * page + lane] = scale;
   }
 }
 
 // One stage in ring slot S: write it, load the stage kStages ahead, and after the
 // barrier compute the wave's steps of it.
 template <int D, int TW, int NE, int NW, bool kFp8, int S>
-__device__ __forceinline__ void tree_ring_step(const TreeRing &c, char *ring, int b, int wave,
-                                               int lane, TreeStage<D, NW, kFp8> &r,
+__device__ __forceinline__ void tree_ring_step(const TreeRing &c, char *ring, float *vscales,
+                                               int b, int wave,
+                                               int lane, TreeStage<D, kFp8> &r,
                                                const TreeQ<D, TW> &qv, const Role &role,
                                                float scale_log2, RowState<TW, NE> &st) {
   using R = Ring<D, NW>;
   char *stage = ring + S * R::kStage;
-  tree_ring_store<D, NW, kFp8>(stage, wave, lane, r);
-  tree_ring_load<D, NW, kFp8>(c, b + R::kStages, wave, r);
+  float *vscale = vscales + S * R::kKeys;
+  tree_ring_store<D, NW, kFp8>(c, b, stage, vscale, wave, lane, r);
+  tree_ring_load<D, kFp8>(c, b + R::kStages, r);
   __syncthreads();
   if (c.sb + b * R::kKeys >= c.prio_end) __builtin_amdgcn_s_setprio(0);
   if (!role.active) return;
@@ -515,35 +481,35 @@ __device__ __forceinline__ void tree_ring_step(const TreeRing &c, char *ring, in
 #pragma unroll
     for (int u = 0; u < NE; ++u)
       v.x[u] = *reinterpret_cast<const u32x4 *>(vb + sub * 2 * R::kTile + 512 * u);
-    bool odd = false;
-    if (t0 + kBlockKeys > min(c.ctx, c.se)) {
-      tree_mask<TW, NE>(t0, c.se, c.ctx, qv.mask, lane, s, v);
-      odd = any_not_finite(v);
-      if (odd) take_out(v);
-    }
-    step_update<TW, NE>(s, v, scale_log2, st, [&](int t, bf16x8 ph) {
-      if (odd) bring_back(vb + sub * 2 * R::kTile, ph, st.o[t]);
-    });
+    VScales<kFp8> vs;
+    if (kFp8)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        vs.x[h] = *reinterpret_cast<const f32x4 *>(vscale + sub * kBlockKeys + kPage * h + 4 * kq);
+    if (t0 + kBlockKeys > min(c.ctx, c.se))
+      tree_mask<TW>(t0, c.se, c.ctx, qv.mask, lane, s);
+    step_update<TW, NE>(s, v, scale_log2, st, vs);
   }
 }
 
 template <int D, int TW, int NE, int NW, bool kFp8>
-__device__ __forceinline__ void tree_ring_run(const TreeRing &c, char *ring, int wave, int lane,
+__device__ __forceinline__ void tree_ring_run(const TreeRing &c, char *ring, float *vscales,
+                                              int wave, int lane,
                                               const TreeQ<D, TW> &qv, const Role &role,
                                               float scale_log2, RowState<TW, NE> &st) {
   constexpr int kStages = Ring<D, NW>::kStages;
-  TreeStage<D, NW, kFp8> r[kStages];
+  TreeStage<D, kFp8> r[kStages];
   // in stage order (the empty asm keeps the compiler from reordering them), so that
   // each step waits only for its own stage
 #pragma unroll
   for (int s = 0; s < kStages; ++s) {
-    tree_ring_load<D, NW, kFp8>(c, s, wave, r[s]);
+    tree_ring_load<D, kFp8>(c, s, r[s]);
     asm volatile("" ::: "memory");
   }
   for (int b = 0; b < c.ns; b += kStages) {
-    tree_ring_step<D, TW, NE, NW, kFp8, 0>(c, ring, b, wave, lane, r[0], qv, role, scale_log2, st);
-    tree_ring_step<D, TW, NE, NW, kFp8, 1>(c, ring, b + 1, wave, lane, r[1], qv, role, scale_log2, st);
-    tree_ring_step<D, TW, NE, NW, kFp8, 2>(c, ring, b + 2, wave, lane, r[2], qv, role, scale_log2, st);
+    tree_ring_step<D, TW, NE, NW, kFp8, 0>(c, ring, vscales, b, wave, lane, r[0], qv, role, scale_log2, st);
+    tree_ring_step<D, TW, NE, NW, kFp8, 1>(c, ring, vscales, b + 1, wave, lane, r[1], qv, role, scale_log2, st);
+    tree_ring_step<D, TW, NE, NW, kFp8, 2>(c, ring, vscales, b + 2, wave, lane, r[2], qv, role, scale_log2, st);
   }
 }
 
@@ -579,11 +545,43 @@ __device__ __forceinline__ void write_tree_rows(const TreeParams &p, const TreeP
   }
 }
 
+// Adds the V cells of the piece's nodes that are not finite, which the ring left out, to
+// the rows that see them.
+template <int D, int TW, int NE, bool kFp8>
+__device__ __forceinline__ void add_not_finite(const TreeParams &p, const TreePiece &x,
+                                               const Role &role, int lane,
+                                               const unsigned long long (&mask)[TW],
+                                               RowState<TW, NE> &st) {
+  const int kq = lane >> 4;
+#pragma unroll 1
+  for (int key = max(x.key_begin, x.rq.ctx); key < x.key_end; ++key) {
+    const int id = p.page_table[(size_t)x.i * p.max_pages + key / kPage];
+    const size_t page = (unsigned)id < (unsigned)p.num_pages ? id : 0;
+    const size_t tile = ((page * 2 + 1) * p.hkv + x.g) * kPage * D + key % kPage;
+#pragma unroll
+    for (int u = 0; u < NE; ++u)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const size_t at = tile + (size_t)(16 * (role.e_lo + u) + 4 * kq + q) * kPage;
+        float v = 0.f;
+        if constexpr (kFp8)
+          v = (((const uint8_t *)p.kv)[at] & 0x7F) == 0x7F ? NAN : 0.f;
+        else
+          v = __uint_as_float((uint32_t)((const uint16_t *)p.kv)[at] << 16);
+        if (fabsf(v) < INFINITY) continue;
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+          if (mask[t] >> (key - x.rq.ctx) & 1) st.o[t][u][q] += v;
+      }
+  }
+}
+
 // Wave roles as run_piece in attn.hip: with NE < D/16 d blocks the waves split one
 // tile's dims (or two tiles', half of the waves each), else each has TW tiles to itself.
 template <int D, int TW, int NE, int NW, bool kFp8>
-__device__ __forceinline__ void run_tree_piece(const TreeParams &p, char *buf, int *ids,
-                                               const TreePiece &x, int wave, int lane) {
+__device__ __forceinline__ void run_tree_piece(const TreeParams &p, char *buf, float *vscales,
+                                               int *not_finite, const TreePiece &x,
+                                               int wave, int lane) {
   using R = Ring<D, NW>;
   constexpr int kParts = D / 16 / NE;  // waves to a tile
   constexpr int kCell = kFp8 ? 1 : 2;
@@ -596,33 +594,30 @@ __device__ __forceinline__ void run_tree_piece(const TreeParams &p, char *buf, i
   load_tree_q<D, TW>(p, x, role.tile0, lane, qv);
   clear_state<TW, NE>(st);
   TreeRing c;
-  c.ids = ids;
+  const int kind = wave & 1;
   c.page_bytes = (uint32_t)(2 * p.hkv * kPage * D * kCell);
-  c.kbase = reinterpret_cast<const char *>(p.kv) + (size_t)x.g * kPage * D * kCell + 16 * lane;
-  c.vbase = reinterpret_cast<const char *>(p.kv) + (size_t)(p.hkv + x.g) * kPage * D * kCell +
-            16 * (kFp8 ? lane : v_unit_inv(lane));
-  c.scales = p.scales + (size_t)x.g * 2 * kPage;
+  c.base = reinterpret_cast<const char *>(p.kv) + (size_t)(kind * p.hkv + x.g) * kPage * D * kCell +
+           16 * (!kFp8 && kind ? v_unit_inv(lane) : lane);
+  c.scales = p.scales + (size_t)x.g * 2 * kPage + kind * kPage + (lane & 15);
   c.scale_bytes = (uint32_t)(p.hkv * 2 * kPage);
   c.ctx = x.rq.ctx;
   c.prio_end = x.prio_end;
-  for (int sb = x.key_begin; sb < x.key_end; sb += kSubKeys) {
-    const int se = min(x.key_end, sb + kSubKeys);
+  c.not_finite = not_finite;
+  if (threadIdx.x == 0) *not_finite = 0;
+  __syncthreads();
+  constexpr int kSub = 64 * kIdRegs * R::kKeys;
+  for (int sb = x.key_begin; sb < x.key_end; sb += kSub) {
     c.sb = sb;
-    c.se = se;
-    c.ns = (se - sb + R::kKeys - 1) / R::kKeys;
-    // an id outside [0, num_pages) breaks the contract and reads page 0 instead; pages
-    // past the sub-piece read page 0 and are masked
-    const int npg = (se - sb + kPage - 1) / kPage;
-    const int32_t *pt = p.page_table + (size_t)x.i * p.max_pages + sb / kPage;
-    if (sb > x.key_begin) __syncthreads();  // the last ids and stages have been read
-    for (int t = threadIdx.x; t < R::kPages * c.ns; t += NW * kWave) {
-      const int id = t < npg ? pt[t] : 0;
-      ids[t] = (unsigned)id < (unsigned)p.num_pages ? id : 0;
-    }
-    __syncthreads();
-    tree_ring_run<D, TW, NE, NW, kFp8>(c, buf, wave, lane, qv, role, p.scale_log2, st);
+    c.se = min(x.key_end, sb + kSub);
+    c.ns = (c.se - sb + R::kKeys - 1) / R::kKeys;
+    load_ids<NW>(p, x.i, wave, lane, c);
+    if (sb > x.key_begin) __syncthreads();  // the last stages have been read
+    tree_ring_run<D, TW, NE, NW, kFp8>(c, buf, vscales, wave, lane, qv, role, p.scale_log2, st);
   }
   if (!role.active) return;
+  // set, if at all, before the last stage's barrier
+  if (__builtin_amdgcn_readfirstlane(*not_finite) != 0)
+    add_not_finite<D, TW, NE, kFp8>(p, x, role, lane, qv.mask, st);
 #pragma unroll
   for (int t = 0; t < TW; ++t)
     write_tree_rows<D, NE>(p, x, role.tile0 + t, role.e_lo, lane, st.m[t], row_sum4(st.l[t]),
@@ -637,7 +632,8 @@ template <int D, int NW, int kTW, bool kFp8>
 __global__ __launch_bounds__(NW *kWave, tree_waves_per_simd(D, NW, kTW)) void tree_attn_kernel(
     TreeParams p) {
   __shared__ __attribute__((aligned(1024))) char buf[Ring<D, NW>::kBytes];
-  __shared__ int ids[kSubPages];
+  __shared__ __attribute__((aligned(16))) float vscales[kFp8 ? Ring<D, NW>::kStages * Ring<D, NW>::kKeys : 4];
+  __shared__ int not_finite;
   __shared__ int lds_plan[2 * NW + 8 + (kNumPieceCaps / 2 + 2) * NW];
 
   const TreeShare sh = tree_plan<D, NW>(p, lds_plan);
@@ -683,15 +679,15 @@ __global__ __launch_bounds__(NW *kWave, tree_waves_per_simd(D, NW, kTW)) void tr
     const int nt = (x.rows + 15) / 16;  // row tiles
     constexpr int kBlocks = D / 16;
     if (NW == 4 && nt == 1)
-      run_tree_piece<D, 1, kBlocks / 4, NW, kFp8>(p, buf, ids, x, wave, lane);
+      run_tree_piece<D, 1, kBlocks / 4, NW, kFp8>(p, buf, vscales, &not_finite, x, wave, lane);
     else if (NW == 4 && nt == 2)
-      run_tree_piece<D, 1, kBlocks / 2, NW, kFp8>(p, buf, ids, x, wave, lane);
+      run_tree_piece<D, 1, kBlocks / 2, NW, kFp8>(p, buf, vscales, &not_finite, x, wave, lane);
     else if (kTW == 1 || nt <= NW)
-      run_tree_piece<D, 1, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+      run_tree_piece<D, 1, kBlocks, NW, kFp8>(p, buf, vscales, &not_finite, x, wave, lane);
     else if (kTW == 2 || nt <= 2 * NW)
-      run_tree_piece<D, 2, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+      run_tree_piece<D, 2, kBlocks, NW, kFp8>(p, buf, vscales, &not_finite, x, wave, lane);
     else
-      run_tree_piece<D, kTW, kBlocks, NW, kFp8>(p, buf, ids, x, wave, lane);
+      run_tree_piece<D, kTW, kBlocks, NW, kFp8>(p, buf, vscales, &not_finite, x, wave, lane);
 
     pos += take;
     off += take;
