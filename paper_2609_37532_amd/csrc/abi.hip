@@ -553,7 +553,7 @@ int dsv_kv_read(const void *kv_pages, const void *kv_scales, int32_t kv_dtype,
   if (rc != DSV_OK) return rc;
   if (!aligned16(k_out) || !aligned16(v_out)) return DSV_ERR_UNSUPPORTED;
   const ReadParams p = {kv_pages, (const uint8_t *)kv_scales, kv_refs, k_out, v_out,
-                        rows,     num_kv_heads,               num_pages};
+                        rows,     num_kv_heads,               num_pages, 0};
   const hipError_t e = launch_kv_read(p, head_dim, kv_dtype == DSV_FP8, out_dtype == DSV_F32,
                                       (hipStream_t)hip_stream);
   return e == hipSuccess ? DSV_OK : DSV_ERR_HIP;

@@ -36,6 +36,8 @@ constexpr int kChunk = 16;             // rows in which a workgroup's runs begin
 constexpr int kMaxRows = kChunk + 15;  // rows they can span
 constexpr int kMinExp = -60;           // of a quantised row's scale: tiny rows become 0
 constexpr float kFp8Max = 448.f;
+// From so many (chunk, KV head) pairs on a workgroup takes several heads.
+constexpr int kManyBlocks = 1024, kAppendHeads = 4;
 
 // Chunk of a K tile: dims of one slot that lie together.
 template <bool kFp8>
@@ -170,52 +172,60 @@ __device__ __forceinline__ void any_dims(int rot, int p, int &da, int &db) {
   db = 2 * p < rot ? p + rot / 2 : 2 * p + 1;
 }
 
+// Sixteen values as they lie in memory: two vectors of eight dims.
 template <bool kF32>
-__device__ __forceinline__ void load8(const void *row, int d, float (&x)[8]) {
-  if (kF32) {
-    const f32x4 *v = reinterpret_cast<const f32x4 *>((const float *)row + d);
-    const f32x4 u = v[0], w = v[1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = u[e];
-      x[4 + e] = w[e];
-    }
-  } else {
-    const u32x4 v = *reinterpret_cast<const u32x4 *>((const uint16_t *)row + d);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = bf16_lo(v[e]);
-      x[2 * e + 1] = bf16_hi(v[e]);
-    }
-  }
-}
+struct Raw {
+  u32x4 x[kF32 ? 4 : 2];
+};
 template <bool kF32>
-__device__ __forceinline__ float load1(const void *row, int d) {
-  return kF32 ? ((const float *)row)[d]
-              : __uint_as_float((uint32_t)((const uint16_t *)row)[d] << 16);
-}
-
-template <bool kF32>
-__device__ __forceinline__ void load_pairs(const void *row, int mode, int rot, int t,
-                                           float (&a)[8], float (&b)[8]) {
+__device__ __forceinline__ void load_raw(const void *row, int mode, int rot, int t, Raw<kF32> &r) {
+  constexpr int kBytes = kF32 ? 4 : 2;
   if (mode == kHalfAny) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       int da, db;
       any_dims(rot, 8 * t + e, da, db);
-      a[e] = load1<kF32>(row, da);
-      b[e] = load1<kF32>(row, db);
+      if constexpr (kF32) {
+        r.x[e / 4][e % 4] = ((const uint32_t *)row)[da];
+        r.x[2 + e / 4][e % 4] = ((const uint32_t *)row)[db];
+      } else {
+        r.x[e / 4][e % 4] = (uint32_t)((const uint16_t *)row)[da] |
+                            (uint32_t)((const uint16_t *)row)[db] << 16;
+      }
     }
     return;
   }
   const PairDims d = pair_dims(mode, rot, t);
-  float u[8], w[8];
-  load8<kF32>(row, d.a, u);
-  load8<kF32>(row, mode == kHalfVec ? d.b : d.a + 8, w);
+  const char *a = (const char *)row + d.a * kBytes;
+  const char *b = (const char *)row + (mode == kHalfVec ? d.b : d.a + 8) * kBytes;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    a[e] = mode == kHalfVec ? u[e] : (e < 4 ? u[2 * (e & 3)] : w[2 * (e & 3)]);
-    b[e] = mode == kHalfVec ? w[e] : (e < 4 ? u[2 * (e & 3) + 1] : w[2 * (e & 3) + 1]);
+  for (int q = 0; q < (kF32 ? 2 : 1); ++q) {
+    r.x[q] = *reinterpret_cast<const u32x4 *>(a + 16 * q);
+    r.x[(kF32 ? 2 : 1) + q] = *reinterpret_cast<const u32x4 *>(b + 16 * q);
+  }
+}
+// As pairs.
+template <bool kF32>
+__device__ __forceinline__ void pairs_of(const Raw<kF32> &r, int mode, float (&a)[8], float (&b)[8]) {
+  if constexpr (kF32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // two vectors of a, then b; or sixteen dims in order
+      const float pa = __uint_as_float(r.x[e / 4][e % 4]), pb = __uint_as_float(r.x[2 + e / 4][e % 4]);
+      const float qa = __uint_as_float(r.x[e / 2][2 * (e % 2)]);
+      const float qb = __uint_as_float(r.x[e / 2][2 * (e % 2) + 1]);
+      a[e] = mode == kAdjacent ? qa : pa;
+      b[e] = mode == kAdjacent ? qb : pb;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // a word of each vector holds two dims of it; or a pair (kHalfAny likewise)
+      const uint32_t wa = r.x[0][e / 2], wb = r.x[1][e / 2], w = r.x[e / 4][e % 4];
+      const float pa = e % 2 ? bf16_hi(wa) : bf16_lo(wa), pb = e % 2 ? bf16_hi(wb) : bf16_lo(wb);
+      a[e] = mode == kHalfVec ? pa : bf16_lo(w);
+      b[e] = mode == kHalfVec ? pb : bf16_hi(w);
+    }
   }
 }
 
@@ -306,6 +316,24 @@ __device__ void append_kv(const AppendParams &p, char *lds, int block, int live)
   // stage row - row
   const int shift = (__builtin_amdgcn_readlane(x.ref, x.first) & (kPage - 1)) - x.first;
   const int half = p.rot / 2;
+  // item n: thread n % kTph of a row's K, then of the rows' V; the first one of a head is
+  // loaded ahead, under the angles and under the head before
+  auto load_item = [&](int n, int g, Raw<kF32> &r) {
+    const bool is_v = n >= nr * kTph;
+    const int at = is_v ? n - nr * kTph : n;
+    const int l = x.first + at / kTph;
+    if (n >= 2 * nr * kTph || !x.owns(l)) return;
+    const char *src = (const char *)(is_v ? p.v : p.k) +
+                      ((size_t)(r0 + l) * (size_t)(is_v ? p.v_stride : p.k_stride) + (size_t)g * D) *
+                          (kF32 ? 4 : 2);
+    load_raw<kF32>(src, is_v ? (int)kAdjacent : p.mode, p.rot, at % kTph, r);
+  };
+  // every head's first item is loaded ahead, under the angles
+  Raw<kF32> ahead[kAppendHeads];
+#pragma unroll
+  for (int h = 0; h < kAppendHeads; ++h)
+    if (g0 + h < g1) load_item(threadIdx.x, g0 + h, ahead[h]);
+#pragma unroll 1
   for (int n = threadIdx.x; n < nr * half; n += kThreads) {
     const int r = n / half, i = n - r * half;
     double s, c;
@@ -314,25 +342,29 @@ __device__ void append_kv(const AppendParams &p, char *lds, int block, int live)
   }
   __syncthreads();
   const size_t tile = (size_t)kPage * D;
+#pragma unroll 1
   for (int g = g0; g < g1; ++g) {
     if (g > g0) __syncthreads();  // the last head's stage has been read
+    Raw<kF32> item = ahead[0];
+#pragma unroll
+    for (int h = 1; h < kAppendHeads; ++h)
+      if (g == g0 + h) item = ahead[h];
+#pragma unroll 1
     for (int n = threadIdx.x; n < 2 * nr * kTph; n += kThreads) {
       const bool is_v = n >= nr * kTph;
       const int at = is_v ? n - nr * kTph : n;
       const int l = x.first + at / kTph, t = at % kTph;
+      if (n >= kThreads) load_item(n, g, item);
       if (!x.owns(l)) continue;
-      const size_t row = (size_t)(r0 + l);
-      const char *src = (const char *)(is_v ? p.v : p.k) +
-                        (row * (size_t)(is_v ? p.v_stride : p.k_stride) + (size_t)g * D) *
-                            (kF32 ? 4 : 2);
       const int mode = is_v ? (int)kAdjacent : p.mode;
       float a[8], b[8];
-      load_pairs<kF32>(src, mode, p.rot, t, a, b);
+      pairs_of<kF32>(item, mode, a, b);
       if (!is_v) {
         const double2 *turn = cs + (l - x.first) * (D / 2) + 8 * t;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (8 * t + e < half) {
+            asm volatile("" ::: "memory");  // one pair's factors at a time: 120 registers less
             const double2 w = turn[e];
             const double u = a[e], v = b[e];
             a[e] = to_odd(__builtin_fma(u, w.x, -(v * w.y)));
@@ -426,6 +458,7 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
   const int nr = min(p.q_rows, live - r0);
   if (nr <= 0) return;
   const int half = p.rot / 2;
+#pragma unroll 1
   for (int n = threadIdx.x; n < nr * half; n += kThreads) {
     const int r = n / half, i = n - r * half;
     double s, c;
@@ -434,14 +467,26 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
                                       (float)(s * (double)p.rope_scale));
   }
   __syncthreads();
-  const int per_row = p.hq * kTph;
-  for (int r = 0; r < nr; ++r)
-    for (int n = threadIdx.x; n < per_row; n += kThreads) {
-      const int h = n / kTph, t = n % kTph;
-      const size_t row = (size_t)(r0 + r);
-      const char *src = (const char *)p.q + (row * (size_t)p.q_stride + (size_t)h * D) * (kF32 ? 4 : 2);
+  // four items of a thread in flight at a time
+  const int per_row = p.hq * kTph, total = nr * per_row;
+  constexpr int kItems = 4;
+  for (int n0 = threadIdx.x; n0 < total; n0 += kItems * kThreads) {
+    Raw<kF32> raw[kItems];
+#pragma unroll
+    for (int y = 0; y < kItems; ++y) {
+      const int n = n0 + y * kThreads, r = n / per_row, i = n - r * per_row;
+      if (n >= total) continue;
+      const char *src = (const char *)p.q + ((size_t)(r0 + r) * (size_t)p.q_stride +
+                                             (size_t)(i / kTph) * D) * (kF32 ? 4 : 2);
+      load_raw<kF32>(src, p.mode, p.rot, i % kTph, raw[y]);
+    }
+#pragma unroll
+    for (int y = 0; y < kItems; ++y) {
+      const int n = n0 + y * kThreads, r = n / per_row, i = n - r * per_row;
+      if (n >= total) continue;
+      const int h = i / kTph, t = i % kTph;
       float a[8], b[8];
-      load_pairs<kF32>(src, p.mode, p.rot, t, a, b);
+      pairs_of<kF32>(raw[y], p.mode, a, b);
       const float2 *turn = cs + r * (D / 2) + 8 * t;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -453,7 +498,7 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
         }
       uint32_t w[8];
       bf16_words(p.mode, a, b, w);
-      uint16_t *out = p.q_out + (row * p.hq + h) * D;
+      uint16_t *out = p.q_out + ((size_t)(r0 + r) * p.hq + h) * D;
       if (p.mode == kHalfAny) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -469,6 +514,7 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
             u32x4{w[4], w[5], w[6], w[7]};
       }
     }
+  }
 }
 
 // Workgroups [0, kv_blocks) write the cache, the others rotate q.
@@ -498,45 +544,48 @@ __device__ __forceinline__ void fp8_values(u32x4 w, float scale, float (&x)[16])
 }
 __device__ __forceinline__ float scale_of(uint8_t e) { return __uint_as_float((uint32_t)e << 23); }
 
+// Eight values to eight dims of an output row.
 template <bool kF32>
-__device__ __forceinline__ void store16(void *row, int d, const float (&x)[16]) {
+__device__ __forceinline__ void store8(void *row, int d, const float (&x)[8]) {
   if (kF32) {
     f32x4 *to = reinterpret_cast<f32x4 *>((float *)row + d);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) to[q] = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    to[0] = f32x4{x[0], x[1], x[2], x[3]};
+    to[1] = f32x4{x[4], x[5], x[6], x[7]};
   } else {
-    u32x4 *to = reinterpret_cast<u32x4 *>((uint16_t *)row + d);
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      to[q] = u32x4{pack_bf16x2(x[8 * q], x[8 * q + 1]), pack_bf16x2(x[8 * q + 2], x[8 * q + 3]),
-                    pack_bf16x2(x[8 * q + 4], x[8 * q + 5]), pack_bf16x2(x[8 * q + 6], x[8 * q + 7])};
+    *reinterpret_cast<u32x4 *>((uint16_t *)row + d) =
+        u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+              pack_bf16x2(x[6], x[7])};
   }
 }
 
+constexpr int kReadHeads = 4;  // most KV heads to a workgroup
 template <bool kFp8, bool kF32, int D>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
   constexpr int kTph = D / 16;
-  constexpr int kPitch = D + 4;
-  __shared__ __attribute__((aligned(16))) float rows[kMaxRows * kPitch];  // V
+  using Out = typename std::conditional<kF32, float, uint16_t>::type;
+  constexpr int kPitch = D + 16 / sizeof(Out);  // rows 16 bytes apart in the banks
+  __shared__ __attribute__((aligned(16))) Out rows[(kF32 ? 1 : kReadHeads) * kMaxRows * kPitch];  // V
   __shared__ int run_row[kChunk], refs[kMaxRows];
   const int lane = threadIdx.x % kWave;
   const int chunks = (p.rows + kChunk - 1) / kChunk;
-  const int r0 = blockIdx.x % chunks * kChunk, g = blockIdx.x / chunks;
+  const int r0 = blockIdx.x % chunks * kChunk, g0 = blockIdx.x / chunks * p.heads_per_block;
+  const int heads = min(p.heads_per_block, p.hkv - g0);
   const Runs x = find_runs(p.refs, r0, p.rows, p.num_pages * kPage, lane);
   const size_t tile = (size_t)kPage * D;
-  const size_t es = kF32 ? 4 : 2;
-  auto out_row = [&](void *base, int l) {
-    return (char *)base + ((size_t)(r0 + l) * p.hkv + g) * D * es;
+  auto out_row = [&](void *base, int l, int h) {
+    return (Out *)base + ((size_t)(r0 + l) * p.hkv + g0 + h) * D;
   };
   // rows of this chunk without a slot in the cache
-  for (int n = threadIdx.x; n < kChunk * kTph; n += kThreads) {
-    const int l = n / kTph, t = n % kTph;
-    if (r0 + l >= p.rows || (x.valid >> l & 1)) continue;
-    const float zero[16] = {};
-    store16<kF32>(out_row(p.k_out, l), 16 * t, zero);
-    store16<kF32>(out_row(p.v_out, l), 16 * t, zero);
-  }
+  if (((unsigned)~x.valid & ((1u << kChunk) - 1)) != 0)
+    for (int n = threadIdx.x; n < heads * kChunk * (D / 8); n += kThreads) {
+      const int l = n / (D / 8) % kChunk, h = n / (D / 8 * kChunk), d = n % (D / 8) * 8;
+      if (r0 + l >= p.rows || (x.valid >> l & 1)) continue;
+      const float zero[8] = {};
+      store8<kF32>(out_row(p.k_out, l, h), d, zero);
+      store8<kF32>(out_row(p.v_out, l, h), d, zero);
+    }
   if (x.first == x.end) return;
+  const int nr = x.end - x.first;
   const unsigned starts = (unsigned)x.start & ((1u << kChunk) - 1);
   const int num_runs = __builtin_popcount(starts);
   if ((int)threadIdx.x < kChunk && (starts >> lane & 1))
@@ -544,19 +593,25 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
   if ((int)threadIdx.x < kMaxRows) refs[lane] = x.ref;
   __syncthreads();
   // V: a thread takes one dim of a run, 16 slots at once, into rows
-  for (int n = threadIdx.x; n < num_runs * D; n += kThreads) {
-    const int l = run_row[n / D], d = n % D;
+  for (int n = threadIdx.x; n < heads * num_runs * D; n += kThreads) {
+    const int d = n % D, h = n / D % heads, l = run_row[n / D / heads];
     const unsigned on = (unsigned)(x.valid & ~x.start);
     const int len = 1 + __builtin_ctz(~(on >> (l + 1)));
     const int ref = refs[l];
     const int page = ref / kPage, slot = ref % kPage;
-    const size_t at = ((size_t)page * 2 * p.hkv + p.hkv + g) * tile + (size_t)d * kPage;
-    float *to = rows + (l - x.first) * kPitch + d;
-    const uint8_t *sc = kFp8 ? p.scales + (((size_t)page * p.hkv + g) * 2 + 1) * kPage : nullptr;
+    const size_t at = ((size_t)page * 2 * p.hkv + p.hkv + g0 + h) * tile + (size_t)d * kPage;
+    Out *to = rows + (h * kMaxRows + l - x.first) * kPitch + d;
+    auto put = [&](int row, float v) {
+      if constexpr (kF32)
+        to[row * kPitch] = v;
+      else
+        to[row * kPitch] = (uint16_t)(__float_as_uint(v) >> 16);  // exact: bf16 holds it
+    };
+    const uint8_t *sc = kFp8 ? p.scales + (((size_t)page * p.hkv + g0 + h) * 2 + 1) * kPage : nullptr;
     if (len == 1) {
-      to[0] = kFp8 ? __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)p.pages)[at + slot], 0) *
-                         scale_of(sc[slot])
-                   : __uint_as_float((uint32_t)((const uint16_t *)p.pages)[at + slot] << 16);
+      put(0, kFp8 ? __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)p.pages)[at + slot], 0) *
+                        scale_of(sc[slot])
+                  : __uint_as_float((uint32_t)((const uint16_t *)p.pages)[at + slot] << 16));
       continue;
     }
     float v[16];
@@ -577,49 +632,57 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
         v[8 + 2 * q + 1] = bf16_hi(hi[q]);
       }
     }
+    if (len == kPage) {
 #pragma unroll
-    for (int q = 0; q < 16; ++q)
-      if (q >= slot && q < slot + len) to[(q - slot) * kPitch] = v[q];
+      for (int q = 0; q < 16; ++q) put(q, v[q]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; ++q)
+        if (q >= slot && q < slot + len) put(q - slot, v[q]);
+    }
   }
-  // K: a thread takes sixteen dims of a row
-  for (int n = threadIdx.x; n < (x.end - x.first) * kTph; n += kThreads) {
-    const int l = x.first + n / kTph, t = n % kTph;
+  // K: a thread takes sixteen dims of a row; a wave eight rows of a head, whose chunks and
+  // output rows lie together
+  for (int n = threadIdx.x; n < heads * nr * kTph; n += kThreads) {
+    const int t = n % kTph, l = x.first + n / kTph % nr, h = n / kTph / nr;
     if (!x.owns(l)) continue;
     const int ref = refs[l];
     const int page = ref / kPage, slot = ref % kPage;
-    const size_t at = ((size_t)page * 2 * p.hkv + g) * tile;
-    float v[16];
+    const size_t at = ((size_t)page * 2 * p.hkv + g0 + h) * tile;
+    u32x4 w[2];
+    float lo[8], hi[8];
     if constexpr (kFp8) {
-      const u32x4 w = *reinterpret_cast<const u32x4 *>((const uint8_t *)p.pages + at +
-                                                       (size_t)(t * kPage + slot) * 16);
-      fp8_values(w, scale_of(p.scales[((size_t)page * p.hkv + g) * 2 * kPage + slot]), v);
+      w[0] = *reinterpret_cast<const u32x4 *>((const uint8_t *)p.pages + at +
+                                              (size_t)(t * kPage + slot) * 16);
+      float v[16];
+      fp8_values(w[0], scale_of(p.scales[((size_t)page * p.hkv + g0 + h) * 2 * kPage + slot]), v);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        lo[q] = v[q];
+        hi[q] = v[8 + q];
+      }
     } else {
       const uint16_t *k = (const uint16_t *)p.pages + at;
-      const u32x4 lo = *reinterpret_cast<const u32x4 *>(k + (size_t)(2 * t * kPage + slot) * 8);
-      const u32x4 hi = *reinterpret_cast<const u32x4 *>(k + (size_t)((2 * t + 1) * kPage + slot) * 8);
+      w[0] = *reinterpret_cast<const u32x4 *>(k + (size_t)(2 * t * kPage + slot) * 8);
+      w[1] = *reinterpret_cast<const u32x4 *>(k + (size_t)((2 * t + 1) * kPage + slot) * 8);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        v[2 * q] = bf16_lo(lo[q]);
-        v[2 * q + 1] = bf16_hi(lo[q]);
-        v[8 + 2 * q] = bf16_lo(hi[q]);
-        v[8 + 2 * q + 1] = bf16_hi(hi[q]);
+        lo[2 * q] = bf16_lo(w[0][q]);
+        lo[2 * q + 1] = bf16_hi(w[0][q]);
+        hi[2 * q] = bf16_lo(w[1][q]);
+        hi[2 * q + 1] = bf16_hi(w[1][q]);
       }
     }
-    store16<kF32>(out_row(p.k_out, l), 16 * t, v);
+    store8<kF32>(out_row(p.k_out, l, h), 16 * t, lo);
+    store8<kF32>(out_row(p.k_out, l, h), 16 * t + 8, hi);
   }
   __syncthreads();
-  for (int n = threadIdx.x; n < (x.end - x.first) * kTph; n += kThreads) {
-    const int l = x.first + n / kTph, t = n % kTph;
+  constexpr int kVec = 16 / sizeof(Out);
+  for (int n = threadIdx.x; n < heads * nr * (D / kVec); n += kThreads) {
+    const int d = n % (D / kVec) * kVec, l = x.first + n / (D / kVec) % nr, h = n / (D / kVec) / nr;
     if (!x.owns(l)) continue;
-    const f32x4 *from = reinterpret_cast<const f32x4 *>(rows + (l - x.first) * kPitch + 16 * t);
-    float v[16];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 w = from[q];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * q + e] = w[e];
-    }
-    store16<kF32>(out_row(p.v_out, l), 16 * t, v);
+    *reinterpret_cast<u32x4 *>(out_row(p.v_out, l, h) + d) =
+        *reinterpret_cast<const u32x4 *>(rows + (h * kMaxRows + l - x.first) * kPitch + d);
   }
 }
 
@@ -705,7 +768,7 @@ void (*read_kernel(int dim))(ReadParams) {
 hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipStream_t s) {
   p.mode = p.interleaved || p.rot == 0 ? kAdjacent : (p.rot % 16 == 0 ? kHalfVec : kHalfAny);
   const int chunks = (p.rows + kChunk - 1) / kChunk;
-  p.heads_per_block = (long long)chunks * p.hkv > 1024 ? 4 : 1;
+  p.heads_per_block = (long long)chunks * p.hkv < kManyBlocks ? 1 : kAppendHeads;
   p.kv_blocks = chunks * ((p.hkv + p.heads_per_block - 1) / p.heads_per_block);
   p.q_rows = p.rows >= 2048 ? 4 : 1;
   const int q_blocks = p.hq > 0 ? (p.rows + p.q_rows - 1) / p.q_rows : 0;
@@ -715,11 +778,13 @@ hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipSt
   return hipGetLastError();
 }
 
-hipError_t launch_kv_read(const ReadParams &p, int dim, bool fp8, bool f32, hipStream_t s) {
+hipError_t launch_kv_read(ReadParams p, int dim, bool fp8, bool f32, hipStream_t s) {
   const int chunks = (p.rows + kChunk - 1) / kChunk;
+  p.heads_per_block = f32 || (long long)chunks * p.hkv < kManyBlocks ? 1 : kReadHeads;
+  const int groups = (p.hkv + p.heads_per_block - 1) / p.heads_per_block;
   auto fn = fp8 ? (f32 ? read_kernel<true, true>(dim) : read_kernel<true, false>(dim))
                 : (f32 ? read_kernel<false, true>(dim) : read_kernel<false, false>(dim));
-  launch_kernel(fn, dim3(chunks * p.hkv), dim3(kThreads), s, p);
+  launch_kernel(fn, dim3(chunks * groups), dim3(kThreads), s, p);
   return hipGetLastError();
 }
 

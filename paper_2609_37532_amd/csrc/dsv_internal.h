@@ -144,8 +144,9 @@ struct ReadParams {
   const int32_t *refs;
   void *k_out, *v_out;  // [rows][Hkv][D]
   int32_t rows, hkv, num_pages;
+  int32_t heads_per_block;  // set by the launcher
 };
-hipError_t launch_kv_read(const ReadParams &p, int dim, bool fp8, bool f32, hipStream_t s);
+hipError_t launch_kv_read(ReadParams p, int dim, bool fp8, bool f32, hipStream_t s);
 
 struct CommitParams {
   void *pages;
