@@ -374,47 +374,57 @@ def dvl_allocate_pack(pred_logits, num_live, tokens, positions, kv_refs, k_out, 
 
 
 # ------------------------------------------------- cache rows and drafted trees
-def _require_here(*tensors) -> None:
-    """Every tensor on the current device: a stream of another one would run the
-    kernels there."""
+def _here() -> int:
+    """The current device; without one, a number that no tensor's device has."""
     import torch
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError("tensors must be on the current device (cuda:%d), got %s"
-                             % (here, t.device))
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):
+        return -2
 
 
-def _cache_dtype(kv_pages, kv_scales) -> int:
-    """Checks a cache's tensors; returns its ``kv_dtype``."""
+def _take(t, name: str, dtypes, ndim: int, here: int) -> int:
+    """``_require`` with the device: the kernels run on the current one, and a stream of
+    another would run them there.  Returns the address."""
+    if t.get_device() != here or t.dtype not in dtypes or t.dim() != ndim \
+            or not t.is_contiguous():
+        _require(t, name, dtypes, ndim)
+        raise ValueError("%s must be on the current device (cuda:%d), got %s"
+                         % (name, here, t.device))
+    return t.data_ptr()
+
+
+def _cache(kv_pages, kv_scales, here: int):
+    """Checks a cache's tensors: (kv_dtype, address of the pages, of the scales)."""
     import torch
     if kv_scales is None:
-        _require(kv_pages, "kv_pages", _bf16_like(torch), 4)
-        dtype = DSV_BF16
+        pages = _take(kv_pages, "kv_pages", _bf16_like(torch), 4, here)
+        dtype, scales = DSV_BF16, None
     else:
-        _require(kv_pages, "kv_pages", (torch.uint8, torch.float8_e4m3fn), 4)
-        _require(kv_scales, "kv_scales", (torch.uint8,), 4)
+        pages = _take(kv_pages, "kv_pages", (torch.uint8, torch.float8_e4m3fn), 4, here)
+        scales = _take(kv_scales, "kv_scales", (torch.uint8,), 4, here)
         num_pages, _, hkv, _ = kv_pages.shape
-        if tuple(kv_scales.shape) != (num_pages, hkv, 2, PAGE_SIZE):
+        if kv_scales.shape != (num_pages, hkv, 2, PAGE_SIZE):
             raise ValueError("kv_scales must be [P, Hkv, 2, 16]")
         dtype = DSV_FP8
     if kv_pages.shape[1] != 2 or kv_pages.shape[3] % PAGE_SIZE:
         raise ValueError("kv_pages must be [P, 2, Hkv, 16*D]")
-    return dtype
+    return dtype, pages, scales
 
 
-def _require_rows(t, name: str, dtype, rows: int, dim: int) -> int:
-    """Checks a [rows, heads, dim] tensor with dense heads; returns its row stride."""
-    if not t.is_cuda:
-        raise ValueError("%s must be a device tensor" % name)
+def _take_rows(t, name: str, dtype, rows: int, dim: int, here: int):
+    """Checks a [rows, heads, dim] tensor with dense heads: (address, heads, row stride)."""
+    if t.get_device() != here:
+        raise ValueError("%s must be a device tensor on the current device" % name)
     if t.dtype != dtype:
         raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim:
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != rows or shape[2] != dim:
         raise ValueError("%s must be [%d, heads, %d]" % (name, rows, dim))
-    heads = t.shape[1]
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    heads, stride = shape[1], t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != dim):
         raise ValueError("%s must have dense heads" % name)
-    return t.stride(0) if rows > 1 else heads * dim
+    return t.data_ptr(), heads, stride[0] if rows > 1 else heads * dim
 
 
 def rope_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: Optional[str] = None,
@@ -468,41 +478,42 @@ def rope_append(q, k, v, positions, inv_freq, kv_refs, q_out, kv_pages, kv_scale
     bf16 [rows, Hq, D].  ``inv_freq`` None turns nothing.  ``kv_pages`` bf16, or uint8 with
     ``kv_scales``; ``num_live`` int32 [1] on the device, or None."""
     import torch
-    kv_dtype = _cache_dtype(kv_pages, kv_scales)
-    _require(kv_refs, "kv_refs", (torch.int32,), 1)
-    if k.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("k has dtype %s, expected bfloat16 or float32" % k.dtype)
-    rows, dim = kv_refs.shape[0], kv_pages.shape[3] // PAGE_SIZE
-    hkv = kv_pages.shape[2]
-    ks = _require_rows(k, "k", k.dtype, rows, dim)
-    vs = _require_rows(v, "v", k.dtype, rows, dim)
-    if k.shape[1] != hkv or v.shape[1] != hkv:
+    here, i32 = _here(), (torch.int32,)
+    kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
+    refs = _take(kv_refs, "kv_refs", i32, 1, here)
+    dtype = k.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("k has dtype %s, expected bfloat16 or float32" % dtype)
+    num_pages, _, hkv, tile = kv_pages.shape
+    rows, dim = kv_refs.shape[0], tile // PAGE_SIZE
+    kp, k_heads, ks = _take_rows(k, "k", dtype, rows, dim, here)
+    vp, v_heads, vs = _take_rows(v, "v", dtype, rows, dim, here)
+    if k_heads != hkv or v_heads != hkv:
         raise ValueError("k and v must have the cache's %d heads" % hkv)
+    qp = op = None
     hq = qs = 0
     if q is not None:
-        qs = _require_rows(q, "q", k.dtype, rows, dim)
-        hq = q.shape[1]
-        _require(q_out, "q_out", (torch.bfloat16,), 3)
+        qp, hq, qs = _take_rows(q, "q", dtype, rows, dim, here)
+        op = _take(q_out, "q_out", (torch.bfloat16,), 3, here)
         if q_out.shape != q.shape:
             raise ValueError("q_out must have the shape of q")
-    rot = 0
+    rot, freq, pos = 0, None, None
     if inv_freq is not None:
-        _require(inv_freq, "inv_freq", (torch.float32,), 1)
-        _require(positions, "positions", (torch.int32,), 1)
+        freq = _take(inv_freq, "inv_freq", (torch.float32,), 1, here)
+        pos = _take(positions, "positions", i32, 1, here)
         if positions.shape[0] != rows:
             raise ValueError("positions must have %d entries" % rows)
         rot = 2 * inv_freq.shape[0]
+    live = None
     if num_live is not None:
-        _require(num_live, "num_live", (torch.int32,), 1)
+        live = _take(num_live, "num_live", i32, 1, here)
         if num_live.shape[0] != 1:
             raise ValueError("num_live must hold one int32")
-    _require_here(q, k, v, q_out, kv_refs, kv_pages, kv_scales, positions, inv_freq, num_live)
-    dims = AppendDims(rows, hq, hkv, dim, PAGE_SIZE, kv_pages.shape[0],
-                      DSV_BF16 if k.dtype == torch.bfloat16 else DSV_F32, kv_dtype, rot,
-                      1 if interleaved else 0, float(rope_scale), qs, ks, vs)
+    dims = AppendDims(rows, hq, hkv, dim, PAGE_SIZE, num_pages,
+                      DSV_BF16 if dtype == torch.bfloat16 else DSV_F32, kv_dtype, rot,
+                      1 if interleaved else 0, rope_scale, qs, ks, vs)
     _check("dsv_rope_append", load().dsv_rope_append(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(inv_freq), _ptr(kv_refs),
-        _ptr(num_live), _ptr(q_out), _ptr(kv_pages), _ptr(kv_scales), ctypes.byref(dims),
+        qp, kp, vp, pos, freq, refs, live, op, pages, scales, ctypes.byref(dims),
         _stream_handle(stream)))
 
 
@@ -510,17 +521,17 @@ def kv_read(kv_pages, kv_refs, k_out, v_out, kv_scales=None, *, stream=None) -> 
     """Enqueue ``dsv_kv_read``: the cache rows of the slots ``kv_refs`` (int32 [rows]) into
     k_out, v_out [rows, Hkv, D], bf16 or float32."""
     import torch
-    kv_dtype = _cache_dtype(kv_pages, kv_scales)
-    _require(kv_refs, "kv_refs", (torch.int32,), 1)
-    _require(k_out, "k_out", (torch.bfloat16, torch.float32), 3)
-    _require(v_out, "v_out", (k_out.dtype,), 3)
+    here = _here()
+    kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
+    refs = _take(kv_refs, "kv_refs", (torch.int32,), 1, here)
+    kp = _take(k_out, "k_out", (torch.bfloat16, torch.float32), 3, here)
+    vp = _take(v_out, "v_out", (k_out.dtype,), 3, here)
     num_pages, _, hkv, tile = kv_pages.shape
     want = (kv_refs.shape[0], hkv, tile // PAGE_SIZE)
-    if tuple(k_out.shape) != want or tuple(v_out.shape) != want:
+    if k_out.shape != want or v_out.shape != want:
         raise ValueError("k_out and v_out must be [%d, %d, %d]" % want)
-    _require_here(kv_pages, kv_refs, k_out, v_out, kv_scales)
     _check("dsv_kv_read", load().dsv_kv_read(
-        _ptr(kv_pages), _ptr(kv_scales), kv_dtype, _ptr(kv_refs), _ptr(k_out), _ptr(v_out),
+        pages, scales, kv_dtype, refs, kp, vp,
         DSV_BF16 if k_out.dtype == torch.bfloat16 else DSV_F32, want[0], hkv, want[2], PAGE_SIZE,
         num_pages, _stream_handle(stream)))
 
@@ -529,20 +540,20 @@ def tree_masks(parents, cu_qlens, ctx_lens, masks, positions=None, *, stream=Non
     """Enqueue ``dsv_tree_masks``: ``parents`` int32 [cap] to ``masks`` int64 [cap] (the
     bits of each node and its ancestors) and ``positions`` int32 [cap] or None."""
     import torch
-    for t, n in ((parents, "parents"), (cu_qlens, "cu_qlens"), (ctx_lens, "ctx_lens")):
-        _require(t, n, (torch.int32,), 1)
-    _require(masks, "masks", (torch.int64, torch.uint64), 1)
-    cap, B = parents.shape[0], ctx_lens.shape[0]
+    here, i32 = _here(), (torch.int32,)
+    up = _take(parents, "parents", i32, 1, here)
+    cu = _take(cu_qlens, "cu_qlens", i32, 1, here)
+    ctx = _take(ctx_lens, "ctx_lens", i32, 1, here)
+    mp = _take(masks, "masks", (torch.int64, torch.uint64), 1, here)
+    cap, B, pos = parents.shape[0], ctx_lens.shape[0], None
     if positions is not None:
-        _require(positions, "positions", (torch.int32,), 1)
+        pos = _take(positions, "positions", i32, 1, here)
         if positions.shape[0] != cap:
             raise ValueError("positions must be [cap]")
     if masks.shape[0] != cap or cu_qlens.shape[0] != B + 1:
         raise ValueError("masks must be [cap], cu_qlens [B+1] and ctx_lens [B]")
-    _require_here(parents, cu_qlens, ctx_lens, masks, positions)
-    _check("dsv_tree_masks", load().dsv_tree_masks(
-        _ptr(parents), _ptr(cu_qlens), _ptr(ctx_lens), _ptr(masks), _ptr(positions), B, cap,
-        _stream_handle(stream)))
+    _check("dsv_tree_masks", load().dsv_tree_masks(up, cu, ctx, mp, pos, B, cap,
+                                                   _stream_handle(stream)))
 
 
 def tree_attn_dims(q_packed, kv_pages, page_table, kv_scales=None, *, max_nodes: int = MAX_NODES,
@@ -565,40 +576,39 @@ def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv
     """Enqueue ``dsv_tree_attn``: q_packed, out bf16 [cap, Hq, D]; ``masks`` int64 [cap]
     (of ``tree_masks``) or None (causal); ``kv_pages`` bf16, or uint8 with ``kv_scales``."""
     import torch
-    bf = _bf16_like(torch)
-    kv_dtype = _cache_dtype(kv_pages, kv_scales)
-    _require(q_packed, "q_packed", bf, 3)
-    _require(out, "out", bf, 3)
-    _require(cu_qlens, "cu_qlens", (torch.int32,), 1)
-    _require(page_table, "page_table", (torch.int32,), 2)
-    _require(ctx_lens, "ctx_lens", (torch.int32,), 1)
+    here, i32, bf = _here(), (torch.int32,), _bf16_like(torch)
+    kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
+    q = _take(q_packed, "q_packed", bf, 3, here)
+    o = _take(out, "out", bf, 3, here)
+    cu = _take(cu_qlens, "cu_qlens", i32, 1, here)
+    table = _take(page_table, "page_table", i32, 2, here)
+    ctx = _take(ctx_lens, "ctx_lens", i32, 1, here)
     if dims is None:
         dims = tree_attn_dims(q_packed, kv_pages, page_table, kv_scales, max_nodes=max_nodes,
                               max_kv_len=max_kv_len, scale=scale)
     cap, hq, dim = q_packed.shape
+    num_pages, _, hkv, tile = kv_pages.shape
+    B, pmax = page_table.shape
     # dims made for other tensors would reach past these
-    if (dims.capacity, dims.num_q_heads, dims.head_dim) != (cap, hq, dim) or \
-            (dims.num_pages, dims.num_kv_heads) != (kv_pages.shape[0], kv_pages.shape[2]) or \
-            kv_pages.shape[3] != PAGE_SIZE * dim or dims.kv_dtype != kv_dtype or \
-            (dims.num_reqs, dims.max_pages_per_req) != tuple(page_table.shape):
+    if (dims.capacity, dims.num_q_heads, dims.head_dim, dims.num_pages, dims.num_kv_heads,
+            dims.kv_dtype, dims.num_reqs, dims.max_pages_per_req) != (
+            cap, hq, dim, num_pages, hkv, kv_dtype, B, pmax) or tile != PAGE_SIZE * dim:
         raise ValueError("dims do not belong to these tensors")
     if out.shape != q_packed.shape:
         raise ValueError("out must have the shape of q_packed")
-    B = dims.num_reqs
     if cu_qlens.shape[0] != B + 1 or ctx_lens.shape[0] != B:
         raise ValueError("cu_qlens must have B+1 entries and ctx_lens B")
+    mp = None
     if masks is not None:
-        _require(masks, "masks", (torch.int64, torch.uint64), 1)
+        mp = _take(masks, "masks", (torch.int64, torch.uint64), 1, here)
         if masks.shape[0] != cap:
             raise ValueError("masks must be [cap]")
     if workspace is None:
         workspace = alloc_workspace(tree_attn_workspace_bytes(dims), q_packed.device)
-    _require_here(q_packed, cu_qlens, masks, kv_pages, kv_scales, page_table, ctx_lens, out,
-                  workspace)
+    ws = _take(workspace, "workspace", (torch.uint8,), 1, here)
     _check("dsv_tree_attn", load().dsv_tree_attn(
-        _ptr(q_packed), _ptr(cu_qlens), _ptr(masks), _ptr(kv_pages), _ptr(kv_scales),
-        _ptr(page_table), _ptr(ctx_lens), _ptr(out), ctypes.byref(dims), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+        q, cu, mp, pages, scales, table, ctx, o, ctypes.byref(dims), ws, workspace.shape[0],
+        _stream_handle(stream)))
 
 
 def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path, next_token, *,
@@ -606,24 +616,23 @@ def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path
     """Enqueue ``dsv_tree_accept``; logits float32 or bfloat16 [cap, vocab], ``parents`` and
     ``path`` int32 [cap]; the workspace is ``accept``'s."""
     import torch
-    _require(logits_packed, "logits_packed", (torch.float32, torch.bfloat16), 2)
+    here, i32 = _here(), (torch.int32,)
+    logits = _take(logits_packed, "logits_packed", (torch.float32, torch.bfloat16), 2, here)
     cap, vocab = logits_packed.shape
     B = cu_qlens.numel() - 1
+    ptrs = []
     for t, n, size in ((cu_qlens, "cu_qlens", B + 1), (draft_tokens, "draft_tokens", cap),
                        (parents, "parents", cap), (accept_len, "accept_len", B),
                        (path, "path", cap), (next_token, "next_token", B)):
-        _require(t, n, (torch.int32,), 1)
+        ptrs.append(_take(t, n, i32, 1, here))
         if t.shape[0] != size:
             raise ValueError("%s must have %d entries" % (n, size))
     if workspace is None:
         workspace = alloc_workspace(accept_workspace_bytes(cap, B, vocab), logits_packed.device)
-    _require_here(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path, next_token,
-                  workspace)
+    ws = _take(workspace, "workspace", (torch.uint8,), 1, here)
     _check("dsv_tree_accept", load().dsv_tree_accept(
-        _ptr(logits_packed), DSV_BF16 if logits_packed.dtype == torch.bfloat16 else DSV_F32,
-        _ptr(cu_qlens), _ptr(draft_tokens), _ptr(parents), _ptr(accept_len), _ptr(path),
-        _ptr(next_token), B, cap, vocab, _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+        logits, DSV_BF16 if logits_packed.dtype == torch.bfloat16 else DSV_F32, *ptrs, B, cap,
+        vocab, ws, workspace.shape[0], _stream_handle(stream)))
 
 
 def tree_commit(kv_pages, cu_qlens, ctx_lens, page_table, path, kv_scales=None, *,
@@ -631,19 +640,19 @@ def tree_commit(kv_pages, cu_qlens, ctx_lens, page_table, path, kv_scales=None, 
     """Enqueue ``dsv_tree_commit``: the accepted path's cache rows of one layer, moved to
     the positions after the context."""
     import torch
-    kv_dtype = _cache_dtype(kv_pages, kv_scales)
-    for t, n in ((cu_qlens, "cu_qlens"), (ctx_lens, "ctx_lens"), (path, "path")):
-        _require(t, n, (torch.int32,), 1)
-    _require(page_table, "page_table", (torch.int32,), 2)
+    here, i32 = _here(), (torch.int32,)
+    kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
+    cu = _take(cu_qlens, "cu_qlens", i32, 1, here)
+    ctx = _take(ctx_lens, "ctx_lens", i32, 1, here)
+    walk = _take(path, "path", i32, 1, here)
+    table = _take(page_table, "page_table", i32, 2, here)
     num_pages, _, hkv, tile = kv_pages.shape
     B, pmax = page_table.shape
     if cu_qlens.shape[0] != B + 1 or ctx_lens.shape[0] != B:
         raise ValueError("cu_qlens must have B+1 entries and ctx_lens B")
-    _require_here(kv_pages, cu_qlens, ctx_lens, page_table, path, kv_scales)
     _check("dsv_tree_commit", load().dsv_tree_commit(
-        _ptr(kv_pages), _ptr(kv_scales), kv_dtype, _ptr(cu_qlens), _ptr(ctx_lens),
-        _ptr(page_table), _ptr(path), B, path.shape[0], hkv, tile // PAGE_SIZE, PAGE_SIZE, pmax,
-        num_pages, _stream_handle(stream)))
+        pages, scales, kv_dtype, cu, ctx, table, walk, B, path.shape[0], hkv, tile // PAGE_SIZE,
+        PAGE_SIZE, pmax, num_pages, _stream_handle(stream)))
 
 
 PROBE_TILE_BYTES = 4096

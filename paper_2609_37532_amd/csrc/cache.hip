@@ -36,7 +36,9 @@ constexpr int kChunk = 16;             // rows in which a workgroup's runs begin
 constexpr int kMaxRows = kChunk + 15;  // rows they can span
 constexpr int kMinExp = -60;           // of a quantised row's scale: tiny rows become 0
 constexpr float kFp8Max = 448.f;
-// From so many (chunk, KV head) pairs on a workgroup takes several heads.
+// From so many (chunk, KV head) pairs on a workgroup takes several heads: two, and from
+// twice as many on four (us a call, 8 KV heads, two / four to a workgroup: 2,047 rows 16.6 /
+// 22.8, 8,191 rows 56.5 / 54.2).
 constexpr int kManyBlocks = 1024, kAppendHeads = 4;
 
 // Chunk of a K tile: dims of one slot that lie together.
@@ -768,7 +770,8 @@ void (*read_kernel(int dim))(ReadParams) {
 hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipStream_t s) {
   p.mode = p.interleaved || p.rot == 0 ? kAdjacent : (p.rot % 16 == 0 ? kHalfVec : kHalfAny);
   const int chunks = (p.rows + kChunk - 1) / kChunk;
-  p.heads_per_block = (long long)chunks * p.hkv < kManyBlocks ? 1 : kAppendHeads;
+  const long long pairs = (long long)chunks * p.hkv;
+  p.heads_per_block = pairs < kManyBlocks ? 1 : (pairs < 2 * kManyBlocks ? 2 : kAppendHeads);
   p.kv_blocks = chunks * ((p.hkv + p.heads_per_block - 1) / p.heads_per_block);
   p.q_rows = p.rows >= 2048 ? 4 : 1;
   const int q_blocks = p.hq > 0 ? (p.rows + p.q_rows - 1) / p.q_rows : 0;
