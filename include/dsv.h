@@ -417,7 +417,7 @@ int dsv_dvl_allocate_pack(const float *pred_logits, const int32_t *num_live,
 /*
  * Dimensions of one rope_append call.  All fields are host values.
  *
- *  rows           rows of q, k and v, >= 1.
+ *  rows           rows of q, k and v, 1 .. 2^24; rows * num_kv_heads <= 2^27.
  *  num_q_heads    Hq >= 0 (0: no q; q and q_out are not used).
  *  num_kv_heads   Hkv >= 1.
  *  head_dim       D in {64, 128}.
@@ -492,7 +492,8 @@ int dsv_rope_append(const void *q, const void *k, const void *v, const int32_t *
  * be named any number of times.  Exact (an 8-bit cache's values fit bf16).
  *   kv_pages, kv_scales  the bf16 (kv_dtype DSV_BF16, kv_scales NULL) or 8-bit cache.
  *   k_out, v_out         bf16 or fp32 (out_dtype) [rows][Hkv][D].
- * All but kv_refs must be 16-byte aligned.  rows >= 1, num_pages * 16 < 2^31.
+ * All but kv_refs must be 16-byte aligned.  rows >= 1, rows * num_kv_heads <= 2^27,
+ * num_pages * 16 < 2^31.
  */
 int dsv_kv_read(const void *kv_pages, const void *kv_scales, int32_t kv_dtype,
                 const int32_t *kv_refs, void *k_out, void *v_out, int32_t out_dtype,

@@ -42,6 +42,9 @@ int check_dims(const dsv_attn_dims *d) {
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
+// Rows times KV heads of one call on cache rows: a grid has fewer than 2^32 threads.
+constexpr long long kMaxHeadRows = 1LL << 27;
+
 // Head dim, page size and page count of a cache that slots are named in.
 int check_cache(int32_t num_kv_heads, int32_t head_dim, int32_t page_size, int32_t num_pages,
                 int32_t kv_dtype) {
@@ -493,7 +496,7 @@ int dsv_rope_append(const void *q, const void *k, const void *v, const int32_t *
   if (d.rows < 1 || d.rows > (1 << 24) || d.num_q_heads < 0 || d.num_q_heads > 65535 ||
       d.rotary_dim < 0 || d.rotary_dim > d.head_dim || d.rotary_dim % 2 != 0 ||
       (d.interleaved != 0 && d.interleaved != 1) || !isfinite(d.rope_scale) ||
-      (long long)d.rows * d.num_kv_heads > (1LL << 30))
+      (long long)d.rows * d.num_kv_heads > kMaxHeadRows)
     return DSV_ERR_DIMS;
   if (d.in_dtype != DSV_BF16 && d.in_dtype != DSV_F32) return DSV_ERR_UNSUPPORTED;
   if ((d.num_q_heads > 0 && (!q || !q_out)) || (d.rotary_dim > 0 && (!positions || !inv_freq)))
@@ -546,8 +549,7 @@ int dsv_kv_read(const void *kv_pages, const void *kv_scales, int32_t kv_dtype,
   if (!kv_refs || !k_out || !v_out) return DSV_ERR_NULL;
   int rc = check_cache(num_kv_heads, head_dim, page_size, num_pages, kv_dtype);
   if (rc != DSV_OK) return rc;
-  if (rows < 1 || rows > (1 << 30) || (long long)rows * num_kv_heads > (1LL << 33))
-    return DSV_ERR_DIMS;
+  if (rows < 1 || (long long)rows * num_kv_heads > kMaxHeadRows) return DSV_ERR_DIMS;
   if (out_dtype != DSV_BF16 && out_dtype != DSV_F32) return DSV_ERR_UNSUPPORTED;
   rc = check_pages(kv_pages, kv_scales, kv_dtype);
   if (rc != DSV_OK) return rc;

@@ -471,7 +471,7 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
   __syncthreads();
   // four items of a thread in flight at a time
   const int per_row = p.hq * kTph, total = nr * per_row;
-  constexpr int kItems = 4;
+  constexpr int kItems = kF32 ? 2 : 4;
   for (int n0 = threadIdx.x; n0 < total; n0 += kItems * kThreads) {
     Raw<kF32> raw[kItems];
 #pragma unroll

@@ -79,6 +79,7 @@ def append_call(dims, **kw):
     ("page_size", 32, -3), ("num_pages", 0, -2), ("num_pages", 2 ** 27, -2), ("in_dtype", 2, -3),
     ("kv_dtype", 0, -3), ("rotary_dim", 130, -2), ("rotary_dim", 7, -2), ("interleaved", 2, -2),
     ("rope_scale", float("nan"), -2), ("q_stride", 1016, -2), ("q_stride", 1028, -3),
+    ("rows", 2 ** 24 + 1, -2), ("num_kv_heads", 2 ** 27, -2), ("num_kv_heads", -1, -2),
     ("k_stride", 248, -2), ("v_stride", 260, -3), ("k_stride", 2 ** 41, -2)])
 def test_append_refuses_dims(field, value, status):
     assert append_call(append_dims(**{field: value})) == status
@@ -104,7 +105,7 @@ def read_call(**kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(pages=None), -1), (dict(scales=None), -1), (dict(refs=None), -1), (dict(k=None), -1),
     (dict(v=None), -1), (dict(kv_dtype=0), -3), (dict(kv_dtype=1), -3), (dict(out=2), -3),
-    (dict(rows=0), -2), (dict(hkv=0), -2), (dict(dim=80), -3), (dict(page=8), -3),
+    (dict(rows=0), -2), (dict(hkv=0), -2), (dict(rows=2 ** 26 + 1), -2), (dict(dim=80), -3), (dict(page=8), -3),
     (dict(pages_n=0), -2), (dict(v=FAKE + 2), -3), (dict(scales=FAKE + 4), -3)])
 def test_read_refuses(kw, status):
     assert read_call(**kw) == status
