@@ -26,6 +26,27 @@
 //    holds dims of one slot, so K's scale goes into the conversion instruction; V's lane
 //    holds the slots of one dim, so V's scales, through LDS, go into the fp32 weights.
 //    Both are powers of two: exact.
+//
+// What bounds it, and what it measured (MI355X, split + combine kernels, us a call):
+//   B=32, 32/8 heads, contexts to 8K, bf16 cache (0.6 GB): one node 105, 5.7 TB/s (HBM);
+//     16 nodes (4 row tiles) 121; 32 nodes (8) 159; 64 nodes (16) 287: from five tiles on
+//     the matrix products and the softmax of the waves, which share their barriers and
+//     so their phases: at 64 nodes the vector units are busy 46% and the matrix units
+//     35% of the time, and hardly at once.
+//   The same with the 8-bit cache (0.3 GB): 92, 107, 156, 284.  One to four tiles are bound
+//     by instruction issue: four waves of which each does the softmax of its rows for its
+//     own dims (with no products the loads and conversions take 62).
+//   B=16, 64/8 heads, 64 nodes, contexts to 16K, bf16 (0.25 PFLOP): 459, 0.55 PFLOP/s
+//     counting each product once (the weights' second half adds another half).
+//   B=1, 16 nodes, context 700: 12.2 + 4.2, the chain from launch to the last block.
+// Tried, and slower: each wave streaming blocks of its own straight into the operands'
+// registers, no LDS and no barriers (64 nodes: 1,438; the four-tile form spills, and loads
+// that land in accumulation registers are waited for at once; D = 64, which does not spill,
+// 209 against 164); one wave per SIMD with four tiles (500); six stages in flight
+// (8-bit, 24 nodes: 245 against 140, spills); the tiles of a request dealt evenly with a
+// branch for each (10 tiles 228 against 239, 16 tiles 309 against 293: the branch keeps one
+// tile's products from running under another's softmax); neighbouring shares on one
+// XCD, and cached loads, for several row groups (490 either way).
 #include "attn_core.h"
 
 #include <atomic>
@@ -386,18 +407,21 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, float scale) {
 // on, that lie past the keys or are not finite, and notes the latter.
 template <bool kFp8>
 __device__ __forceinline__ u32x4 only_finite(u32x4 x, int key, int se, int *not_finite) {
-  bool found = false;
+  // in integer arithmetic on whole words: conditions by cell would take scalar registers
+  // that the key loop needs (8-bit cache, one node: 90 us a call with them, 78 without)
+  constexpr int kPer = kFp8 ? 4 : 2, kBits = 32 / kPer;  // cells of a word, bits of a cell
+  constexpr uint32_t kSpecial = kFp8 ? 0x7F7F7F7Fu : 0x7F807F80u;  // a cell's bits if not finite
+  constexpr uint32_t kOne = kFp8 ? 0x01010101u : 0x00800080u;      // carries those to its top bit
+  constexpr uint32_t kTop = kFp8 ? 0x80808080u : 0x80008000u;
+  uint32_t found = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    constexpr int kPer = kFp8 ? 4 : 2;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) {
-      const uint32_t cell = kFp8 ? 0xFFu << (8 * c) : 0xFFFFu << (16 * c);
-      const uint32_t special = kFp8 ? 0x7Fu << (8 * c) : 0x7F80u << (16 * c);
-      const bool in = key + kPer * w + c < se, odd = (x[w] & special) == special;
-      found |= in && odd;
-      x[w] &= in && !odd ? 0xFFFFFFFFu : ~cell;
-    }
+    const int cells = min(max(se - key - kPer * w, 0), kPer);  // before the end
+    const uint32_t keep = (uint32_t)((1ull << (kBits * cells)) - 1);
+    const uint32_t top = ((x[w] & kSpecial) + kOne) & kTop;
+    const uint32_t odd = (top - (top >> (kBits - 1))) | top;  // whole cells
+    found |= odd & keep;
+    x[w] &= keep & ~odd;
   }
   if (found) *not_finite = 1;
   return x;
@@ -826,7 +850,9 @@ __global__ __launch_bounds__(kWave) void tree_masks_kernel(const int32_t *parent
 }
 
 // The split kernel for a batch's dims: as many row tiles as the largest tree has, up to
-// what a workgroup's registers hold.
+// what a workgroup's registers hold.  D = 128: four waves of one or two tiles, two
+// workgroups to a CU; above eight tiles eight waves of two, one to a CU.  D = 64: four waves
+// of one, two or four tiles, four, three and two workgroups to a CU.
 struct TreeKernel {
   int index;  // of the form, below kTreeKernels
   void (*fn)(TreeParams);
