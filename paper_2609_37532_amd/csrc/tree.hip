@@ -327,8 +327,11 @@ __device__ __forceinline__ void tree_mask(int t0, int se, int ctx,
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (!(seen >> (16 * h + q) & 1)) s.x[t][h][q] = -INFINITY;
+      for (int q = 0; q < 4; ++q) {
+        // in integers, as in only_finite
+        const uint32_t keep = (uint32_t)((int)(seen << (31 - 16 * h - q)) >> 31);
+        s.x[t][h][q] = __uint_as_float((__float_as_uint(s.x[t][h][q]) & keep) | (0xFF800000u & ~keep));
+      }
   }
 }
 
