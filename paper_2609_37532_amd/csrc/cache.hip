@@ -467,6 +467,14 @@ __device__ void append_kv(const AppendParams &p, char *lds, int block, int live)
   }
 }
 
+// Dense outputs go past the L2 caches, which the kernels' other traffic uses and a reader
+// on another XCD does not (kv_read of 60,001 rows 84.6 -> 78.1 us, append of 8,191 54.5 ->
+// 51.7).
+__device__ __forceinline__ void store16(void *to, u32x4 x) {
+  __builtin_nontemporal_store(x, reinterpret_cast<u32x4 *>(to));
+}
+
+
 template <bool kF32, int D>
 __device__ void append_q(const AppendParams &p, char *lds, int block, int live) {
   constexpr int kTph = D / 16;
@@ -526,9 +534,8 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
         }
       } else {
         const PairDims d = pair_dims(p.mode, p.rot, t);
-        *reinterpret_cast<u32x4 *>(out + d.a) = u32x4{w[0], w[1], w[2], w[3]};
-        *reinterpret_cast<u32x4 *>(out + (p.mode == kHalfVec ? d.b : d.a + 8)) =
-            u32x4{w[4], w[5], w[6], w[7]};
+        store16(out + d.a, u32x4{w[0], w[1], w[2], w[3]});
+        store16(out + (p.mode == kHalfVec ? d.b : d.a + 8), u32x4{w[4], w[5], w[6], w[7]});
       }
     }
   }
@@ -565,23 +572,25 @@ __device__ __forceinline__ float scale_of(uint8_t e) { return __uint_as_float((u
 template <bool kF32>
 __device__ __forceinline__ void store8(void *row, int d, const float (&x)[8]) {
   if (kF32) {
-    f32x4 *to = reinterpret_cast<f32x4 *>((float *)row + d);
-    to[0] = f32x4{x[0], x[1], x[2], x[3]};
-    to[1] = f32x4{x[4], x[5], x[6], x[7]};
+    const f32x4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
+    store16((float *)row + d, __builtin_bit_cast(u32x4, lo));
+    store16((float *)row + d + 4, __builtin_bit_cast(u32x4, hi));
   } else {
-    *reinterpret_cast<u32x4 *>((uint16_t *)row + d) =
-        u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-              pack_bf16x2(x[6], x[7])};
+    store16((uint16_t *)row + d,
+            u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                  pack_bf16x2(x[6], x[7])});
   }
 }
 
-constexpr int kReadHeads = 4;  // most KV heads to a workgroup
+// Most KV heads to a workgroup (60,001 8-bit rows, one / two / four heads: D = 128 95 / 78 /
+// 85 us, D = 64 - / 48 / 42).
+constexpr int read_heads(int dim) { return 256 / dim; }
 template <bool kFp8, bool kF32, int D>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
   constexpr int kTph = D / 16;
   using Out = typename std::conditional<kF32, float, uint16_t>::type;
   constexpr int kPitch = D + 16 / sizeof(Out);  // rows 16 bytes apart in the banks
-  __shared__ __attribute__((aligned(16))) Out rows[(kF32 ? 1 : kReadHeads) * kMaxRows * kPitch];  // V
+  __shared__ __attribute__((aligned(16))) Out rows[(kF32 ? 1 : read_heads(D)) * kMaxRows * kPitch];  // V
   __shared__ int run_row[kChunk], refs[kMaxRows];
   const int lane = threadIdx.x % kWave;
   const int chunks = (p.rows + kChunk - 1) / kChunk;
@@ -698,8 +707,8 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
   for (int n = threadIdx.x; n < heads * nr * (D / kVec); n += kThreads) {
     const int d = n % (D / kVec) * kVec, l = x.first + n / (D / kVec) % nr, h = n / (D / kVec) / nr;
     if (!x.owns(l)) continue;
-    *reinterpret_cast<u32x4 *>(out_row(p.v_out, l, h) + d) =
-        *reinterpret_cast<const u32x4 *>(rows + (h * kMaxRows + l - x.first) * kPitch + d);
+    store16(out_row(p.v_out, l, h) + d,
+            *reinterpret_cast<const u32x4 *>(rows + (h * kMaxRows + l - x.first) * kPitch + d));
   }
 }
 
@@ -798,7 +807,7 @@ hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipSt
 
 hipError_t launch_kv_read(ReadParams p, int dim, bool fp8, bool f32, hipStream_t s) {
   const int chunks = (p.rows + kChunk - 1) / kChunk;
-  p.heads_per_block = f32 || (long long)chunks * p.hkv < kManyBlocks ? 1 : kReadHeads;
+  p.heads_per_block = f32 || (long long)chunks * p.hkv < kManyBlocks ? 1 : read_heads(dim);
   const int groups = (p.hkv + p.heads_per_block - 1) / p.heads_per_block;
   auto fn = fp8 ? (f32 ? read_kernel<true, true>(dim) : read_kernel<true, false>(dim))
                 : (f32 ? read_kernel<false, true>(dim) : read_kernel<false, false>(dim));

@@ -54,7 +54,9 @@
 namespace dsv {
 namespace {
 
-constexpr int kCombThreads = 1024;  // as verify attention's combine
+// Combine kernel (one request of 16 nodes, context 700: 13.6 us a call, with 1,024 threads
+// 15.2; the large batches alike).
+constexpr int kCombThreads = 256;
 
 // Request-level metadata after the device-side checks: seg is ctx + k rounded up to
 // whole blocks, 0 for a request without rows or with metadata out of range; groups its
