@@ -26,16 +26,16 @@
 //    writer rounds.  q is rotated in fp32.
 //
 // What bounds it, and what it measured (MI355X):
-//  * rope_append, 8,191 rows, 32/8 heads, D = 128, bf16 cache (201 MB): 52 us, 3.9 TB/s,
+//  * rope_append, 8,191 rows, 32/8 heads, D = 128, bf16 cache (201 MB): 50 us, 4.1 TB/s,
 //    where a copy of that size reaches 5.4.  q alone takes 31 and the cache alone 31: the
 //    cache writers' chain of slots, angles, four heads' turns and stages, at three
-//    workgroups to a CU.  8-bit cache 51, fp32 inputs 71, D = 64 30 us.  rotary_dim not a
-//    multiple of 16 with the half layout moves by single elements: 144 us.
+//    workgroups to a CU.  8-bit cache 50, fp32 inputs 68, D = 64 27 us.  rotary_dim not a
+//    multiple of 16 with the half layout moves by single elements: 143 us.
 //  * rope_append of one row 5.6 us, of a step's 739 rows 6.6: two round trips (slots, rows),
 //    the angles, a barrier.
-//  * kv_read, 60,001 rows of the 8-bit cache in whole pages (370 MB): 83 us, 4.4 TB/s; 7,500
-//    scattered rows 41 us (each V row costs its whole tile's lines).
-//  * tree_commit: 3.6 us for one request's layer, 4.4 for 32.
+//  * kv_read, 60,001 rows of the 8-bit cache in whole pages (370 MB): 73 us, 5.1 TB/s; 7,500
+//    scattered rows 35 us (each V row costs its whole tile's lines).
+//  * tree_commit: 3.7 us for one request's layer, 4.6 for 32.
 // Tried, and slower: two heads to a pass with K on all four waves (their stages leave a CU
 // two workgroups: 62 us); q in a launch of its own (70); one or eight heads to a
 // workgroup at 8,191 rows (81 before loads ran ahead, 56 after).

@@ -28,22 +28,22 @@
 //    Both are powers of two: exact.
 //
 // What bounds it, and what it measured (MI355X, split + combine kernels, us a call):
-//   B=32, 32/8 heads, contexts to 8K, bf16 cache (0.6 GB): one node 105, 5.7 TB/s (HBM);
-//     16 nodes (4 row tiles) 121; 32 nodes (8) 159; 64 nodes (16) 287: from five tiles on
+//   B=32, 32/8 heads, contexts to 8K, bf16 cache (0.6 GB): one node 103, 5.8 TB/s (HBM);
+//     16 nodes (4 row tiles) 120; 32 nodes (8) 157; 64 nodes (16) 283: from five tiles on
 //     the matrix products and the softmax of the waves, which share their barriers and
-//     so their phases: at 64 nodes the vector units are busy 46% and the matrix units
-//     35% of the time, and hardly at once.
-//   The same with the 8-bit cache (0.3 GB): 92, 107, 156, 284.  One to four tiles are bound
+//     so their phases.
+//   The same with the 8-bit cache (0.3 GB): 78, 97, 146, 270.  One to four tiles are bound
 //     by instruction issue: four waves of which each does the softmax of its rows for its
 //     own dims (with no products the loads and conversions take 62).
-//   B=16, 64/8 heads, 64 nodes, contexts to 16K, bf16 (0.25 PFLOP): 459, 0.55 PFLOP/s
-//     counting each product once (the weights' second half adds another half).
-//   B=1, 16 nodes, context 700: 12.2 + 4.2, the chain from launch to the last block.
+//   B=16, 64/8 heads, 32 to 64 nodes, contexts to 16K, bf16 (0.25 TFLOP): 440, 0.57 PFLOP/s
+//     counting each product once (the weights' second half adds another half); the
+//     vector units are busy 37% of the time and the matrix units 35%, hardly at once.
+//   B=1, 16 nodes, context 700: 10.0 + 3.5, the chain from launch to the last block.
 // Tried, and slower: each wave streaming blocks of its own straight into the operands'
 // registers, no LDS and no barriers (64 nodes: 1,438; the four-tile form spills, and loads
 // that land in accumulation registers are waited for at once; D = 64, which does not spill,
-// 209 against 164); one wave per SIMD with four tiles (500); six stages in flight
-// (8-bit, 24 nodes: 245 against 140, spills); the tiles of a request dealt evenly with a
+// 209 against 168); one wave per SIMD with four tiles (500); six stages in flight
+// (8-bit, 24 nodes: 245 against 128, spills); the tiles of a request dealt evenly with a
 // branch for each (10 tiles 228 against 239, 16 tiles 309 against 293: the branch keeps one
 // tile's products from running under another's softmax); neighbouring shares on one
 // XCD, and cached loads, for several row groups (490 either way).
