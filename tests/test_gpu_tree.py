@@ -142,6 +142,32 @@ def test_work_splits(reqs, hkv, ctx, nodes, fp8):
          fp8=fp8).check("split")
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_requests_of_several_row_groups(dim):
+    """More requests than a planning thread's one, some of them cut into row groups."""
+    rng = np.random.default_rng(dim)
+    nodes = rng.integers(0, 4, 530)
+    nodes[rng.permutation(530)[:12]] = rng.integers(17, 40, 12)
+    ctx = rng.integers(0, 60, 530)
+    Case(dim, ctx.tolist(), nodes.tolist(), hkv=1, group=16, dim=dim, fp8=dim == 128).check("many")
+
+
+def test_two_streams_at_once():
+    """Calls that overlap, each with its own workspace."""
+    cases = [Case(31, [900, 40, 3000], [40, 64, 9], fp8=True), Case(32, [2000, 700], [33, 64], group=8)]
+    base = [c.run().out.clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                c.out.fill_(float("nan"))
+                c.run()
+        torch.cuda.synchronize()
+        for c, b in zip(cases, base):
+            assert torch.equal(c.out, b)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("group", [1, 4, 16])
 def test_values_that_are_not_finite_in_unseen_nodes(group, fp8):
@@ -400,3 +426,9 @@ def test_a_tree_step(fp8):
     dsv.tree_attn(q[rows].contiguous(), i32_dev(cu2), None, pages2, tab, cxd, lin, scales2)
     d = (lin.double() - out[rows].double()).abs()
     assert (d <= 2.0 ** -7 * lin.double().abs() + 2.0 ** -10).all()
+    if not fp8:  # the block's own attention reads the cache that rope_append wrote
+        assert k2.max() <= dsv.MAX_QLEN
+        other = torch.empty_like(lin)
+        dsv.verify_attn(q[rows].contiguous(), i32_dev(cu2), pages2, tab, cxd, other)
+        d = (lin.double() - other.double()).abs()
+        assert (d <= 2.0 ** -7 * lin.double().abs() + 2.0 ** -10).all()
