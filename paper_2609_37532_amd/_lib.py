@@ -394,6 +394,18 @@ def _take(t, name: str, dtypes, ndim: int, here: int) -> int:
     return t.data_ptr()
 
 
+def _call_workspace(nbytes: int, device, stream):
+    """A workspace for one call: allocated, cleared and later reused in the order of the
+    stream that the call runs on.  (A call that is captured needs one that its caller
+    keeps.)"""
+    if stream is None:
+        return alloc_workspace(nbytes, device)
+    import torch
+    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    with torch.cuda.stream(s):
+        return alloc_workspace(nbytes, device)
+
+
 def _cache(kv_pages, kv_scales, here: int):
     """Checks a cache's tensors: (kv_dtype, address of the pages, of the scales)."""
     import torch
@@ -574,7 +586,8 @@ def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv
               scale: Optional[float] = None, workspace=None, stream=None,
               dims: Optional[TreeDims] = None) -> None:
     """Enqueue ``dsv_tree_attn``: q_packed, out bf16 [cap, Hq, D]; ``masks`` int64 [cap]
-    (of ``tree_masks``) or None (causal); ``kv_pages`` bf16, or uint8 with ``kv_scales``."""
+    (of ``tree_masks``) or None (causal); ``kv_pages`` bf16, or uint8 with ``kv_scales``.
+    A call that is captured needs ``workspace``."""
     import torch
     here, i32, bf = _here(), (torch.int32,), _bf16_like(torch)
     kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
@@ -604,7 +617,7 @@ def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv
         if masks.shape[0] != cap:
             raise ValueError("masks must be [cap]")
     if workspace is None:
-        workspace = alloc_workspace(tree_attn_workspace_bytes(dims), q_packed.device)
+        workspace = _call_workspace(tree_attn_workspace_bytes(dims), q_packed.device, stream)
     ws = _take(workspace, "workspace", (torch.uint8,), 1, here)
     _check("dsv_tree_attn", load().dsv_tree_attn(
         q, cu, mp, pages, scales, table, ctx, o, ctypes.byref(dims), ws, workspace.shape[0],
@@ -628,7 +641,8 @@ def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path
         if t.shape[0] != size:
             raise ValueError("%s must have %d entries" % (n, size))
     if workspace is None:
-        workspace = alloc_workspace(accept_workspace_bytes(cap, B, vocab), logits_packed.device)
+        workspace = _call_workspace(accept_workspace_bytes(cap, B, vocab), logits_packed.device,
+                                    stream)
     ws = _take(workspace, "workspace", (torch.uint8,), 1, here)
     _check("dsv_tree_accept", load().dsv_tree_accept(
         logits, DSV_BF16 if logits_packed.dtype == torch.bfloat16 else DSV_F32, *ptrs, B, cap,

@@ -168,6 +168,28 @@ def test_two_streams_at_once():
             assert torch.equal(c.out, b)
 
 
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_a_workspace_of_the_calls_own_on_another_stream(as_handle):
+    """Without a workspace argument the call's own is ordered with its stream, whatever
+    the current stream allocates and writes meanwhile."""
+    c = Case(33, [5000, 3000, 40], [64, 20, 9])
+    base = c.run().out.clone()
+    masks = torch.cat([signed(c.masks), torch.zeros(3, dtype=torch.int64, device=DEV)])
+    cu, table, ctx = i32_dev(c.cu), i32_dev(c.table), i32_dev(c.ctx)
+    dims = dsv.tree_attn_dims(c.q, c.pages, table, max_nodes=64, max_kv_len=c.max_len)
+    nbytes = dsv.tree_attn_workspace_bytes(dims)
+    s = torch.cuda.Stream()
+    for _ in range(4):
+        c.out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(3):
+            dsv.tree_attn(c.q, cu, masks, c.pages, table, ctx, c.out, dims=dims,
+                          stream=int(s.cuda_stream) if as_handle else s)
+            torch.full((nbytes + 256,), 255, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, base)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("group", [1, 4, 16])
 def test_values_that_are_not_finite_in_unseen_nodes(group, fp8):
