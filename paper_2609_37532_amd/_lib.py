@@ -627,7 +627,8 @@ def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv
 def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path, next_token, *,
                 workspace=None, stream=None) -> None:
     """Enqueue ``dsv_tree_accept``; logits float32 or bfloat16 [cap, vocab], ``parents`` and
-    ``path`` int32 [cap]; the workspace is ``accept``'s."""
+    ``path`` int32 [cap]; the workspace is ``accept``'s, and a call that is
+    captured needs one."""
     import torch
     here, i32 = _here(), (torch.int32,)
     logits = _take(logits_packed, "logits_packed", (torch.float32, torch.bfloat16), 2, here)
