@@ -555,7 +555,9 @@ size_t dsv_tree_attn_workspace_bytes(const dsv_tree_dims *dims);
  *
  * A row that sees no key (ctx_lens[i] = 0 and an empty mask), or only keys whose
  * score is minus infinity, is zeros.  Bits from k_i on are ignored.  A node that a row
- * does not see has no part in it, also where its K or V hold infinities or NaN.
+ * does not see has no part in it, also where its K or V hold infinities or NaN; a V that a
+ * row sees and that holds one makes its dim of the row not finite (an infinity of the
+ * context may come out as NaN, as in dsv_verify_attn).
  *   masks    uint64 [capacity] (of dsv_tree_masks, or any others), or NULL: row j sees
  *            the nodes up to and including j (the causal block of dsv_verify_attn, for
  *            blocks of up to 64 rows and for the 8-bit cache).

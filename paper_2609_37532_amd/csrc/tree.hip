@@ -19,7 +19,9 @@
 //    weight of 0 times such a V would be NaN in the matrix product.  V cells of node blocks
 //    that are not finite are therefore left out on the way to the ring, as are cells past
 //    the nodes, and noted; a piece that met one adds them, at its end and cell by cell, to
-//    the rows that see them.
+//    the rows that see them: a node's to those with its bit, one of the context, which
+//    shares the block, to all.  (Telling the two apart on the way to the ring took one
+//    request of 16 nodes from 12.9 to 13.4 us a call.)
 //  * An 8-bit cache is half the bytes.  Codes become bf16 on the way from the load
 //    registers to the LDS ring, which is exact, so the ring's layout and all after it are
 //    the bf16 cache's, and each code is converted once for all waves.  A K tile's lane
@@ -409,7 +411,8 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, float scale) {
 }
 
 // Leaves out the cells of a V tile, the lane's sixteen or eight slots of a dim from key
-// on, that lie past the keys or are not finite, and notes the latter.
+// on, that lie past the keys or are not finite, and notes the latter.  (Cells of the context
+// too, where a stage holds both: add_not_finite brings them back.)
 template <bool kFp8>
 __device__ __forceinline__ u32x4 only_finite(u32x4 x, int key, int se, int *not_finite) {
   // in integer arithmetic on whole words: conditions by cell would take scalar registers
@@ -574,16 +577,20 @@ __device__ __forceinline__ void write_tree_rows(const TreeParams &p, const TreeP
   }
 }
 
-// Adds the V cells of the piece's nodes that are not finite, which the ring left out, to
-// the rows that see them.
-template <int D, int TW, int NE, bool kFp8>
+// Adds the V cells that are not finite of the stages in which the ring left them out, to
+// the rows that see them.  Those are the stages from the one on that reaches past the
+// context or past the piece's end (tree_ring_store's condition); every row sees the keys
+// before ctx, also those of a piece that ends inside the context.
+template <int D, int TW, int NE, int NW, bool kFp8>
 __device__ __forceinline__ void add_not_finite(const TreeParams &p, const TreePiece &x,
                                                const Role &role, int lane,
                                                const unsigned long long (&mask)[TW],
                                                RowState<TW, NE> &st) {
-  const int kq = lane >> 4;
+  constexpr int kKeys = Ring<D, NW>::kKeys;  // stages lie at multiples of it from key_begin
+  const int kq = lane >> 4, ctx = x.rq.ctx;
+  const int whole = max(min(ctx, x.key_end) - x.key_begin, 0) / kKeys;  // stages as they are
 #pragma unroll 1
-  for (int key = max(x.key_begin, x.rq.ctx); key < x.key_end; ++key) {
+  for (int key = x.key_begin + whole * kKeys; key < x.key_end; ++key) {
     const int id = p.page_table[(size_t)x.i * p.max_pages + key / kPage];
     const size_t page = (unsigned)id < (unsigned)p.num_pages ? id : 0;
     const size_t tile = ((page * 2 + 1) * p.hkv + x.g) * kPage * D + key % kPage;
@@ -600,7 +607,7 @@ __device__ __forceinline__ void add_not_finite(const TreeParams &p, const TreePi
         if (fabsf(v) < INFINITY) continue;
 #pragma unroll
         for (int t = 0; t < TW; ++t)
-          if (mask[t] >> (key - x.rq.ctx) & 1) st.o[t][u][q] += v;
+          if (key < ctx || (mask[t] >> (key - ctx) & 1)) st.o[t][u][q] += v;
       }
   }
 }
@@ -646,7 +653,7 @@ __device__ __forceinline__ void run_tree_piece(const TreeParams &p, char *buf, f
   if (!role.active) return;
   // set, if at all, before the last stage's barrier
   if (__builtin_amdgcn_readfirstlane(*not_finite) != 0)
-    add_not_finite<D, TW, NE, kFp8>(p, x, role, lane, qv.mask, st);
+    add_not_finite<D, TW, NE, NW, kFp8>(p, x, role, lane, qv.mask, st);
 #pragma unroll
   for (int t = 0; t < TW; ++t)
     write_tree_rows<D, NE>(p, x, role.tile0 + t, role.e_lo, lane, st.m[t], row_sum4(st.l[t]),

@@ -1,0 +1,81 @@
+"""GPU: tree_attn where V of the committed context is not finite.
+
+Every row sees the whole context, so such a cell reaches its dim of every row of the
+request, wherever it lies: beside the nodes, or at the end of a workgroup's piece.  An
+infinity may come out as one or as NaN (a weight enters the product in two parts, of which
+the second may be 0 or negative); the other dims are as without it.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_37532_amd as dsv
+import tree_ref as T
+from gpu_util import i32_dev, say
+from test_gpu_tree import Case
+
+pytestmark = pytest.mark.gpu
+
+
+def poison(c, i, t, dim, bits):
+    """V cell `dim` of position t of request i, in every head: NaN, or these bf16 bits."""
+    page, at = int(c.table[i][t // 16]), T.v_offset(t % 16, dim)
+    if c.fp8:
+        c.pages[page, 1, :, at] = 0x7F
+    else:
+        c.pages.view(torch.int16)[page, 1, :, at] = bits - 65536 if bits > 32767 else bits
+
+
+def check(c, name):
+    say(name, c.ctx, c.nodes, c.hkv, tuple(c.q.shape), c.fp8)
+    c.run()
+    got, want = c.out.double().cpu().numpy(), c.want()
+    finite = np.isfinite(want)
+    assert not finite[:c.live].all()
+    assert np.array_equal(np.isfinite(got), finite)
+    assert np.isnan(got[np.isnan(want)]).all()
+    # test_gpu_tree.py's bound
+    off = np.abs(got[finite] - want[finite])
+    top = np.abs(want[finite]).max(initial=0) + 4.0
+    assert (off <= 2.0 ** -8 * np.abs(want[finite]) + 2.0 ** -10 * top).all()
+    return got
+
+
+FORMS = [(1, 5, 128), (4, 8, 128), (4, 30, 128), (16, 40, 128), (1, 9, 64), (4, 25, 64), (16, 40, 64)]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("masks", ["tree", None])
+@pytest.mark.parametrize("group,nodes,dim", FORMS)
+def test_beside_the_nodes(group, nodes, dim, masks, fp8):
+    c = Case(group + nodes, [97, 700, 33, 1], [nodes, nodes - 1, 3, nodes], hkv=2, group=group, dim=dim,
+             fp8=fp8, masks=masks)
+    for i, ctx in enumerate(c.ctx):
+        for back, d, bits in ((1, 3, 0x7FC0), (20, 17, 0x7F80), (50, 60, 0xFF80)):
+            if ctx >= back:
+                poison(c, i, ctx - back, d, bits)
+    check(c, "beside")
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("group,nodes,dim,ctx", [(4, 16, 128, [3900, 1300]), (16, 64, 128, [3900, 2501]),
+                                                 (4, 64, 128, [3000] * 5), (16, 64, 64, [1900, 1433])])
+def test_in_every_block(group, nodes, dim, ctx, fp8):
+    """One cell in every 32 keys, each in a dim of its own: also in the last ones of a
+    workgroup's piece, wherever the work is cut."""
+    c = Case(nodes, ctx, [nodes] * len(ctx), hkv=1, group=group, dim=dim, fp8=fp8)
+    for i, n in enumerate(ctx):
+        for b in range(n // 32):
+            poison(c, i, 32 * b + (5 * b + i) % 32, b, 0x7FC0)
+    check(c, "blocks")
+
+
+def test_a_causal_block_is_verify_attention_there_too():
+    c = Case(5, [200, 65], [16, 7], masks=None, hkv=2)
+    poison(c, 0, 199, 9, 0x7FC0)
+    poison(c, 1, 40, 100, 0x7F80)
+    got = check(c, "block")
+    other = torch.empty_like(c.out)
+    dsv.verify_attn(c.q, i32_dev(c.cu), c.pages, i32_dev(c.table), i32_dev(c.ctx), other,
+                    max_kv_len=c.max_len)
+    assert np.array_equal(np.isfinite(got), np.isfinite(other.double().cpu().numpy()))
