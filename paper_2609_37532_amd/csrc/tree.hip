@@ -560,12 +560,14 @@ __device__ __forceinline__ void write_tree_rows(const TreeParams &p, const TreeP
     const int at = x.rg * p.group_rows + rr;
     const int j = at >> __builtin_ctz(p.group), hh = at & (p.group - 1);
     const size_t row = (size_t)(x.rq.q0 + j) * p.hq + (size_t)x.g * p.group + hh;
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees no key is 0
+    // a row whose keys have no weight is 0, whatever their values are
+    const float inv = 1.f / l;
+    const uint32_t keep = l == 0.f ? 0u : 0xFFFFFFFFu;
 #pragma unroll
     for (int u = 0; u < NE; ++u) {
       uint2 w;
-      w.x = pack_bf16x2(o[u][0] * inv, o[u][1] * inv);
-      w.y = pack_bf16x2(o[u][2] * inv, o[u][3] * inv);
+      w.x = pack_bf16x2(o[u][0] * inv, o[u][1] * inv) & keep;
+      w.y = pack_bf16x2(o[u][2] * inv, o[u][3] * inv) & keep;
       *reinterpret_cast<uint2 *>(p.out + row * D + dim + 16 * u) = w;
     }
   } else {
@@ -822,10 +824,11 @@ __global__ __launch_bounds__(kCombThreads) void tree_combine_kernel(TreeParams p
       acc += w * o8[u];
     }
   }
-  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const float inv = 1.f / den;
+  const uint32_t keep = den == 0.f ? 0u : 0xFFFFFFFFu;
   uint2 w2;
-  w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+  w2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv) & keep;
+  w2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv) & keep;
   *reinterpret_cast<uint2 *>(p.out + row * D + 4 * d4) = w2;
 }
 

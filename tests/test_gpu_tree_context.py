@@ -79,3 +79,27 @@ def test_a_causal_block_is_verify_attention_there_too():
     dsv.verify_attn(c.q, i32_dev(c.cu), c.pages, i32_dev(c.table), i32_dev(c.ctx), other,
                     max_kv_len=c.max_len)
     assert np.array_equal(np.isfinite(got), np.isfinite(other.double().cpu().numpy()))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("group,nodes,dim,ctx", [(4, 8, 128, 70), (4, 8, 128, 3000), (16, 40, 128, 2000),
+                                                 (16, 40, 64, 1500)])
+def test_a_row_of_scores_of_minus_infinity_is_zeros(group, nodes, dim, ctx, fp8):
+    """Also where V is not finite: none of the values has a weight."""
+    c = Case(nodes + ctx, [ctx, 5], [nodes, 3], hkv=1, group=group, dim=dim, fp8=fp8)
+    at = torch.tensor([T.k_offset(s, 0, fp8) for s in range(16)], device=c.q.device)
+    c.pages[:, 0, :, at] = 0x38 if fp8 else 1.0  # K's dim 0 is positive
+    rows = [(0, 0), (nodes // 2, group - 1), (nodes + 1, 0)]
+    for row, head in rows:
+        c.q[row, head] = 0
+        c.q[row, head, 0] = -float("inf")
+    for i, t in ((0, 0), (0, ctx // 2), (0, ctx - 1), (1, 4)):
+        poison(c, i, t, 7, 0x7FC0)
+    c.run()
+    got = c.out.double().cpu().numpy()
+    for row, head in rows:
+        assert not got[row, head].any() and not np.isnan(got[row, head]).any()
+    others = np.ones(got.shape[:2], bool)
+    others[tuple(zip(*rows))] = False
+    others[c.live:] = False
+    assert np.isnan(got[others][:, 7]).all() and np.isfinite(np.delete(got[others], 7, 1)).all()
