@@ -449,8 +449,9 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: Optiona
     frequency by it; ``"ntk"`` raises the base by factor ** (R / (R - 2)), which leaves the
     fastest frequency and divides the slowest by it; ``"yarn"`` divides the frequencies
     that make at most ``beta_slow`` turns within ``original_len`` positions, keeps those
-    that make ``beta_fast`` or more, blends linearly in the pair's index between, and
-    scales by 0.1 ln(factor) + 1."""
+    that make ``beta_fast`` or more, blends linearly in the pair's index between (from the
+    whole index at or before the one to that at or after the other, which may lie outside
+    the pairs), and scales by 0.1 ln(factor) + 1."""
     import torch
     if rotary_dim < 2 or rotary_dim % 2:
         raise ValueError("rotary_dim must be even and positive")
@@ -471,9 +472,9 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: Optiona
             raise ValueError("yarn scaling needs original_len and beta_fast > beta_slow > 0")
         # the pair index whose frequency makes `turns` turns within original_len
         at = lambda turns: half * math.log(original_len / (2 * math.pi * turns)) / math.log(base)
-        low = min(max(math.floor(at(beta_fast)), 0), half - 1)
-        high = min(max(math.ceil(at(beta_slow)), 0), half - 1)
-        slow = ((i - low) / max(high - low, 1e-3)).clamp(0, 1)
+        # not held within the pairs there are: the slowest may lie inside the ramp
+        low, high = math.floor(at(beta_fast)), math.ceil(at(beta_slow))
+        slow = ((i - low) / (high - low)).clamp(0, 1)
         inv = inv * (1 - slow) + inv / factor * slow
         scale = 0.1 * math.log(factor) + 1.0
     elif scaling not in (None, "ntk"):
