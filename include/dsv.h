@@ -477,9 +477,10 @@ typedef struct {
  *   kv_pages    bf16 (layout of dsv_verify_attn) or 8-bit codes; kv_scales for the
  *               8-bit cache only (NULL otherwise).
  * q, k, v, q_out, kv_pages and kv_scales must be 16-byte aligned.
- * Precision: angles and k's rotation are in double precision, so the one rounding to
- * bf16 or to a code is the exact value's (to 2^-50 of it); q is turned in fp32 and
- * rounded once.  No workspace.
+ * Precision, for angles |theta| <= 2^40: theta is exact, and k is turned in double
+ * precision, to within 2^-50 * (|a| + |b|) * |rope_scale| of the exact value, and rounded
+ * once, to bf16 or to a code; q is turned in fp32, to within 2^-22 * (|a| + |b|) *
+ * |rope_scale|, and rounded once.  No workspace.
  */
 int dsv_rope_append(const void *q, const void *k, const void *v, const int32_t *positions,
                     const float *inv_freq, const int32_t *kv_refs, const int32_t *num_live,

@@ -18,12 +18,13 @@
 //    one page.  A workgroup owns the runs that begin in its 16 rows, whole, up to 15 rows
 //    beyond them; it finds them with a few ballots over the slots.
 //  * V passes through LDS, where it is transposed; K needs no transposing.
-//  * Angles are products of whole positions and fp32 frequencies in double precision,
-//    brought to [-pi/4, pi/4] in two parts of pi/2 and summed as Taylor series, once per
-//    row and frequency for all heads.  k is rotated in double precision too, and brought
-//    to fp32 with its last bit set if anything was cut, so that the one rounding to bf16
-//    or to 8 bits is that of the exact value, and a cache does not depend on how its
-//    writer rounds.  q is rotated in fp32.
+//  * Angles are products of whole positions and fp32 frequencies, exact in two doubles,
+//    brought to [-pi/4, pi/4] in two parts of pi/2 and summed as Taylor series, for each
+//    row and frequency, by each workgroup for its heads.  k is rotated in double precision
+//    too, within 5.5 * 2^-53 * (|a| + |b|) * |scale| of the exact value (2.5 from sin and cos,
+//    one each from their factor, a product and the sum), and brought to fp32 with its last
+//    bit set if anything was cut, so that there is one rounding to bf16 or to 8 bits, and a
+//    cache hardly depends on how its writer rounds.  q is rotated in fp32.
 //
 // What bounds it, and what it measured (MI355X):
 //  * rope_append, 8,191 rows, 32/8 heads, D = 128, bf16 cache (201 MB): 50 us, 4.1 TB/s,
@@ -121,13 +122,17 @@ __device__ __forceinline__ int lead_of(const Runs &x, int lane) {
 }
 
 // ----------------------------------------------------------------------- angles
-// sin and cos of a in double precision, for |a| up to 2^52: n = a / (pi/2) rounded, pi/2 in
-// two parts (106 bits), and the Taylor series of sin and cos to r^17 and r^16, whose
-// remainders at pi/4 are 8e-20 and 2e-18.
-__device__ __forceinline__ void sincos64(double a, double &s, double &c) {
+// sin and cos of the angle position * freq in double precision, each within 2.5 * 2^-53, for
+// angles up to 2^40.  The product has up to 55 bits: a and what its rounding left.  n = a /
+// (pi/2) rounded (the quotient is off by at most 2^-12 there, so r hardly leaves [-pi/4,
+// pi/4]), pi/2 in two parts (106 bits), and the Taylor series of sin and cos to r^17 and r^16,
+// whose remainders at pi/4 are 8e-20 and 2e-18.
+__device__ __forceinline__ void sincos64(int position, float freq, double &s, double &c) {
+  const double p = position, f = freq;
+  const double a = p * f, left = __builtin_fma(p, f, -a);
   const double n = __builtin_rint(a * 0.63661977236758138);
   double r = __builtin_fma(-n, 1.5707963267948966, a);
-  r = __builtin_fma(-n, 6.123233995736766e-17, r);
+  r = __builtin_fma(-n, 6.123233995736766e-17, r) + left;
   const double z = r * r;
   double ps = 1.0 / 355687428096000.0;  // 1/17!
   ps = __builtin_fma(ps, z, -1.0 / 1307674368000.0);
@@ -354,7 +359,7 @@ __device__ void append_kv(const AppendParams &p, char *lds, int block, int live)
   for (int n = threadIdx.x; n < nr * half; n += kThreads) {
     const int r = n / half, i = n - r * half;
     double s, c;
-    sincos64((double)p.pos[r0 + x.first + r] * (double)p.inv_freq[i], s, c);
+    sincos64(p.pos[r0 + x.first + r], p.inv_freq[i], s, c);
     cs[r * (D / 2) + i] = make_double2(c * (double)p.rope_scale, s * (double)p.rope_scale);
   }
   __syncthreads();
@@ -487,7 +492,7 @@ __device__ void append_q(const AppendParams &p, char *lds, int block, int live) 
   for (int n = threadIdx.x; n < nr * half; n += kThreads) {
     const int r = n / half, i = n - r * half;
     double s, c;
-    sincos64((double)p.pos[r0 + r] * (double)p.inv_freq[i], s, c);
+    sincos64(p.pos[r0 + r], p.inv_freq[i], s, c);
     cs[r * (D / 2) + i] = make_float2((float)(c * (double)p.rope_scale),
                                       (float)(s * (double)p.rope_scale));
   }
