@@ -386,6 +386,8 @@ def _here() -> int:
 def _take(t, name: str, dtypes, ndim: int, here: int) -> int:
     """``_require`` with the device: the kernels run on the current one, and a stream of
     another would run them there.  Returns the address."""
+    if t is None:
+        raise ValueError("%s is needed" % name)
     if t.get_device() != here or t.dtype not in dtypes or t.dim() != ndim \
             or not t.is_contiguous():
         _require(t, name, dtypes, ndim)
@@ -426,6 +428,8 @@ def _cache(kv_pages, kv_scales, here: int):
 
 def _take_rows(t, name: str, dtype, rows: int, dim: int, here: int):
     """Checks a [rows, heads, dim] tensor with dense heads: (address, heads, row stride)."""
+    if t is None:
+        raise ValueError("%s is needed" % name)
     if t.get_device() != here:
         raise ValueError("%s must be a device tensor on the current device" % name)
     if t.dtype != dtype:
@@ -494,8 +498,8 @@ def rope_append(q, k, v, positions, inv_freq, kv_refs, q_out, kv_pages, kv_scale
     here, i32 = _here(), (torch.int32,)
     kv_dtype, pages, scales = _cache(kv_pages, kv_scales, here)
     refs = _take(kv_refs, "kv_refs", i32, 1, here)
-    dtype = k.dtype
-    if dtype not in (torch.bfloat16, torch.float32):
+    dtype = None if k is None else k.dtype
+    if k is not None and dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("k has dtype %s, expected bfloat16 or float32" % dtype)
     num_pages, _, hkv, tile = kv_pages.shape
     rows, dim = kv_refs.shape[0], tile // PAGE_SIZE
@@ -633,12 +637,12 @@ def tree_accept(logits_packed, cu_qlens, draft_tokens, parents, accept_len, path
     import torch
     here, i32 = _here(), (torch.int32,)
     logits = _take(logits_packed, "logits_packed", (torch.float32, torch.bfloat16), 2, here)
+    ptrs = [_take(cu_qlens, "cu_qlens", i32, 1, here)]
     cap, vocab = logits_packed.shape
-    B = cu_qlens.numel() - 1
-    ptrs = []
-    for t, n, size in ((cu_qlens, "cu_qlens", B + 1), (draft_tokens, "draft_tokens", cap),
-                       (parents, "parents", cap), (accept_len, "accept_len", B),
-                       (path, "path", cap), (next_token, "next_token", B)):
+    B = cu_qlens.shape[0] - 1
+    for t, n, size in ((draft_tokens, "draft_tokens", cap), (parents, "parents", cap),
+                       (accept_len, "accept_len", B), (path, "path", cap),
+                       (next_token, "next_token", B)):
         ptrs.append(_take(t, n, i32, 1, here))
         if t.shape[0] != size:
             raise ValueError("%s must have %d entries" % (n, size))
