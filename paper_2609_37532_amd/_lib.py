@@ -592,6 +592,7 @@ def tree_attn(q_packed, cu_qlens, masks, kv_pages, page_table, ctx_lens, out, kv
               dims: Optional[TreeDims] = None) -> None:
     """Enqueue ``dsv_tree_attn``: q_packed, out bf16 [cap, Hq, D]; ``masks`` int64 [cap]
     (of ``tree_masks``) or None (causal); ``kv_pages`` bf16, or uint8 with ``kv_scales``.
+    ``max_nodes`` bounds the trees' sizes and chooses the kernel's form: the nearer, the faster.
     A call that is captured needs ``workspace``."""
     import torch
     here, i32, bf = _here(), (torch.int32,), _bf16_like(torch)
@@ -734,7 +735,8 @@ class Graph:
 
 
 class KernelTimer:
-    """HIP-event timing of the library's eager kernel launches."""
+    """HIP-event timing of the eager kernel launches of the verify path, the predictor and
+    DVL (``TIMING_KINDS``; those of trees and cache rows have no kind and are not timed)."""
 
     def __init__(self, max_launches: int = 4096):
         self.max_launches = max_launches

@@ -29,13 +29,17 @@
 // What bounds it, and what it measured (MI355X):
 //  * rope_append, 8,191 rows, 32/8 heads, D = 128, bf16 cache (201 MB): 50 us, 4.1 TB/s,
 //    where a copy of that size reaches 5.4.  q alone takes 31 and the cache alone 31: the
-//    cache writers' chain of slots, angles, four heads' turns and stages, at three
-//    workgroups to a CU.  8-bit cache 50, fp32 inputs 68, D = 64 27 us.  rotary_dim not a
-//    multiple of 16 with the half layout moves by single elements: 143 us.
+//    cache writers' chain of slots, angles, then turns, a stage of V and two barriers for
+//    each head in turn.  8-bit cache (185 MB) 48, fp32 inputs 68, D = 64 27 us: bf16 inputs
+//    hold four workgroups to a CU with a bf16 cache at D = 64 and with an 8-bit one at D =
+//    128, the others three (LDS or registers), and those with four are no nearer to their
+//    floor.  rotary_dim not a multiple of 16 with the half layout moves by single elements:
+//    144 us.
 //  * rope_append of one row 5.6 us, of a step's 739 rows 6.6: two round trips (slots, rows),
 //    the angles, a barrier.
 //  * kv_read, 60,001 rows of the 8-bit cache in whole pages (370 MB): 73 us, 5.1 TB/s; 7,500
-//    scattered rows 35 us (each V row costs its whole tile's lines).
+//    scattered rows 35 us (each V row costs its whole tile's lines).  fp32 outputs, 20,001
+//    rows (205 MB): 62 us, 3.3 TB/s, one head to a workgroup.
 //  * tree_commit: 3.7 us for one request's layer, 4.6 for 32.
 // Tried, and slower: two heads to a pass with K on all four waves (their stages leave a CU
 // two workgroups: 62 us); q in a launch of its own (70); one or eight heads to a
@@ -53,8 +57,12 @@ constexpr int kMaxRows = kChunk + 15;  // rows they can span
 constexpr int kMinExp = -60;           // of a quantised row's scale: tiny rows become 0
 constexpr float kFp8Max = 448.f;
 // From so many (chunk, KV head) pairs on a workgroup takes several heads: two, and from
-// twice as many on four (us a call, 8 KV heads, two / four to a workgroup: 2,047 rows 16.6 /
-// 22.8, 8,191 rows 56.5 / 54.2).
+// twice as many on four.  It saves the angles of the others and loads ahead; below, there
+// are too few workgroups.  us a call, 8 KV heads and 32 query heads, one / two / four heads, a
+// bf16 | an 8-bit cache: 739 rows 9.1 / 12.0 / 19.4 | 9.5 / 13.2 / 21.8; 2,100 rows 16.9 / 16.0 /
+// 22.5 | 15.5 / 17.6 / 25.5; 3,000 21.8 / 20.8 / 23.4 | 20.3 / 19.0 / 26.6; 4,200 29.0 / 26.1 /
+// 24.7 | 26.9 / 24.6 / 27.1; 6,000 42.7 / 37.6 / 36.3 | 38.8 / 34.2 / 33.3; 8,191 58.6 / 51.7 /
+// 49.9 | 55.8 / 49.9 / 48.7.  (An 8-bit cache would change over a little later.)
 constexpr int kManyBlocks = 1024, kAppendHeads = 4;
 
 // Chunk of a K tile: dims of one slot that lie together.
@@ -473,8 +481,8 @@ __device__ void append_kv(const AppendParams &p, char *lds, int block, int live)
 }
 
 // Dense outputs go past the L2 caches, which the kernels' other traffic uses and a reader
-// on another XCD does not (kv_read of 60,001 rows 84.6 -> 78.1 us, append of 8,191 54.5 ->
-// 51.7).
+// on another XCD does not (through them and past them: kv_read of 60,001 8-bit rows 76.9 and
+// 72.4 us, append of 8,191 rows 52.2 and 49.8, into an 8-bit cache 49.3 and 47.8).
 __device__ __forceinline__ void store16(void *to, u32x4 x) {
   __builtin_nontemporal_store(x, reinterpret_cast<u32x4 *>(to));
 }
@@ -589,8 +597,12 @@ __device__ __forceinline__ void store8(void *row, int d, const float (&x)[8]) {
   }
 }
 
-// Most KV heads to a workgroup (60,001 8-bit rows, one / two / four heads: D = 128 95 / 78 /
-// 85 us, D = 64 - / 48 / 42).
+// Most KV heads to a workgroup, from kManyBlocks pairs on: two at D = 128, four at D = 64.  us,
+// one / two / four heads, 8 KV heads in whole pages.  D = 128, 8-bit: 2,000 rows (below
+// kManyBlocks) 4.5 / 5.2 / 7.0, 8,000 10.3 / 11.0 / 13.3, 30,001 31 / 37 / -, 60,001 88 / 72 / -;
+// bf16: 2,000 4.6 / 5.5 / 7.5, 40,001 64 / 65 / 65.  D = 64, 8-bit: 2,000 3.9 / 4.0 / 4.8, 30,001
+// 22.3 / 16.6 / 18.6, 60,001 42 / 30 / 34; bf16: 40,001 28.6 / 27.2 / 28.5.  (So the rule is the
+// largest reads' at D = 128; two heads would do a little better at D = 64.)
 constexpr int read_heads(int dim) { return 256 / dim; }
 template <bool kFp8, bool kF32, int D>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadParams p) {
@@ -804,6 +816,8 @@ hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipSt
   const long long pairs = (long long)chunks * p.hkv;
   p.heads_per_block = pairs < kManyBlocks ? 1 : (pairs < 2 * kManyBlocks ? 2 : kAppendHeads);
   p.kv_blocks = chunks * ((p.hkv + p.heads_per_block - 1) / p.heads_per_block);
+  // one row of q to a workgroup and four: 2,047 rows 15.3 and 15.9 us, 3,000 20.6 and 20.5, 8,191
+  // 58.9 and 49.8 (8-bit cache 50.5 and 47.9)
   p.q_rows = p.rows >= 2048 ? 4 : 1;
   const int q_blocks = p.hq > 0 ? (p.rows + p.q_rows - 1) / p.q_rows : 0;
   auto fn = f32 ? (fp8 ? append_kernel<true, true>(dim) : append_kernel<true, false>(dim))
@@ -814,6 +828,7 @@ hipError_t launch_rope_append(AppendParams p, int dim, bool f32, bool fp8, hipSt
 
 hipError_t launch_kv_read(ReadParams p, int dim, bool fp8, bool f32, hipStream_t s) {
   const int chunks = (p.rows + kChunk - 1) / kChunk;
+  // as fp32 the stage holds one head's V
   p.heads_per_block = f32 || (long long)chunks * p.hkv < kManyBlocks ? 1 : read_heads(dim);
   const int groups = (p.hkv + p.heads_per_block - 1) / p.heads_per_block;
   auto fn = fp8 ? (f32 ? read_kernel<true, true>(dim) : read_kernel<true, false>(dim))

@@ -867,7 +867,12 @@ __global__ __launch_bounds__(kWave) void tree_masks_kernel(const int32_t *parent
 // The split kernel for a batch's dims: as many row tiles as the largest tree has, up to
 // what a workgroup's registers hold.  D = 128: four waves of one or two tiles, two
 // workgroups to a CU; above eight tiles eight waves of two, one to a CU.  D = 64: four waves
-// of one, two or four tiles, four, three and two workgroups to a CU.
+// of one, two or four tiles, four, three and two workgroups to a CU.  The host knows only the
+// bound max_nodes, and trees far below it pay for the larger form.  B=32, 32/8 heads,
+// contexts to 8K, us a call with a bound of the trees' own size and of 64: D = 128, 8-bit
+// cache, 1 node 73 and 115, 8 nodes 83 and 121, 16 nodes 95 and 125, 32 nodes 145 and 161;
+// bf16 100 and 113, 109 and 122, 118 and 129, 151 and 169; D = 64, 8-bit, 1 node 45 and 57, 16
+// nodes 61 and 67; bf16 57 and 59, 68 and 71.
 struct TreeKernel {
   int index;  // of the form, below kTreeKernels
   void (*fn)(TreeParams);
